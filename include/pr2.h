@@ -295,6 +295,152 @@ pr2_status pr2_rollout_layers(const pr2_dims* dims, int32_t L, void* h, const vo
                               float* logits_old, int64_t* near_tie, void* workspace,
                               size_t ws_bytes, int32_t* status_dev, void* stream);
 
+/* ---- training side -----------------------------------------------------------------------
+ * What a step needs beside the layer forward: the policy objective over the vocabulary, the
+ * gradient of the routing and of the token permutation, and the experts' activation kept in
+ * 8 bits between forward and backward.  The paper trains with these objectives (App. A) and gives
+ * no kernels for them.
+ *
+ * These calls take any widths (d, m, V odd or even) and, where a row stride is an argument, any
+ * stride that holds a row.  Tensors in the layer dtype need the alignment of an element and fp32
+ * and int32 ones that of a word; rows that are multiples of 16 bytes apart and start on one run
+ * fastest.  dims->T k is at most 2^30. */
+
+/* Size and constants of one policy-loss call. */
+typedef struct {
+    int64_t T;                  /* tokens (rows of logits)                                      */
+    int64_t V;                  /* vocabulary, 1 <= V <= 2^30                                   */
+    int64_t ld_logits, ld_grad; /* elements between rows (>= V; the columns past V are neither
+                                 * read nor written)                                            */
+    int32_t dtype;              /* of logits and grad (pr2_dtype)                               */
+    uint32_t flags;             /* PR2_F_SYNC_STATUS or 0                                       */
+    float inv_temp;             /* 1 / sampling temperature, > 0                                */
+    float clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high];
+                                 * 0 <= clip_low <= 1, clip_high >= 0                           */
+    float kl_coef;              /* beta >= 0                                                    */
+    float grad_scale;           /* factor of the gradient (not of the loss)                     */
+} pr2_policy_dims;
+
+/*
+ * Clipped policy loss with a KL term, and the gradient of the logits.  Per token t with
+ * z = inv_temp logits[t, :V], a = target[t]:
+ *     lse = log sum_v exp z_v,  logp[t] = z_a - lse,  entropy[t] = lse - sum_v p_v z_v,
+ *     r = exp(logp - logp_old),  L = -min(r A, clip(r) A),            A = advantage[t]
+ *     gap = logp_ref - logp,     K = exp(gap) - gap - 1               (>= 0, 0 when they agree)
+ *     loss[0] = sum_t weight_t (L_t + kl_coef K_t),  loss[1] = sum w L,  loss[2] = sum w K,
+ *     loss[3] = sum_t w_t [the clip shut token t's gradient off]
+ *     grad[t, v] = grad_scale inv_temp c_t ([v = a] - p_v),
+ *     c_t = w_t (kl_coef (1 - exp gap) - (shut ? 0 : r A)).
+ *  logits [T, ld_logits] dtype; target [T] int32; weight [T] fp32 (NULL: 1/T): mask and
+ *    normalisation in one.  A token of weight 0 contributes nothing, whatever its other inputs
+ *    hold (they are not read): logp, entropy and its gradient row are 0.
+ *  advantage [T] fp32; logp_old [T] fp32 (NULL: logp itself, r = 1, an on-policy step);
+ *    logp_ref [T] fp32 (NULL only if kl_coef is 0; K is then 0, also in loss[2]).
+ *  loss [4] fp32 out (summed in double in a fixed order); logp [T], entropy [T] fp32 out, nullable;
+ *  grad [T, ld_grad] dtype out, nullable (no gradient); may be `logits` itself with
+ *    ld_grad = ld_logits (the gradient then overwrites the logits), else the two do not overlap.
+ *  An entry of -inf is a token that cannot be sampled: p = 0, gradient 0.  A row of nothing but
+ *  -inf has no distribution: it contributes nothing, its logp is -inf, its entropy and gradient 0.
+ *  A target outside [0, V) sets PR2_STATUS_BAD_INDEX and counts as a token of weight 0.
+ *  T = 0 writes loss 0.  fp32 arithmetic, the gradient rounded once.  Deterministic.
+ *  workspace: pr2_policy_loss_workspace_bytes(dims) bytes (0: invalid dims), 256-byte aligned.
+ */
+size_t pr2_policy_loss_workspace_bytes(const pr2_policy_dims* dims);
+pr2_status pr2_policy_loss(const pr2_policy_dims* dims, const void* logits, const int32_t* target,
+                           const float* weight, const float* advantage, const float* logp_old,
+                           const float* logp_ref, float* loss, float* logp, float* entropy,
+                           void* grad, void* workspace, size_t ws_bytes, int32_t* status_dev,
+                           void* stream);
+
+/*
+ * Tokens sorted by expert.  The plan is the stable counting sort that pr2_moe_forward makes of
+ * the flat slots f = t k + s (T, d, N <= 256, k <= 32, dtype of dims are used; m is not):
+ *   offsets [N + 1] int32: rows offsets[e] .. offsets[e + 1] - 1 belong to expert e;
+ *   perm [T k] int32: the slot of each row, -1 past offsets[N];
+ *   inv [T k] int32: the row of each slot, -1 for an invalid one (expert outside [0, N) or
+ *     repeated within its token: PR2_STATUS_BAD_INDEX).
+ * Rows:  x[r] = h[perm[r] / k]  ([T k, d] dtype), zero past offsets[N].
+ *  idx [T, k] int32: the plan is made and written.  idx NULL: offsets and inv hold a plan made
+ *    before (perm and the workspace are not used); a later pass sorts rows by the same plan.
+ *  h, x both NULL: the plan alone.  A row number outside [0, T k) in a plan that is given is taken
+ *  as -1, here and in the calls below.
+ *  workspace: pr2_token_sort_workspace_bytes(dims) bytes (0: invalid dims), 256-byte aligned.
+ */
+size_t pr2_token_sort_workspace_bytes(const pr2_dims* dims);
+pr2_status pr2_token_sort(const pr2_dims* dims, const void* h, const int32_t* idx, void* x,
+                          int32_t* offsets, int32_t* perm, int32_t* inv, void* workspace,
+                          size_t ws_bytes, int32_t* status_dev, void* stream);
+
+/* Gradient of the sorted rows w.r.t. the tokens: dh[t] = sum_s dx[inv[t, s]] over the valid slots
+ * in slot order, fp32 sums rounded once.  dx [T k, d], dh [T, d] dtype; rows that no slot names
+ * are not read. */
+pr2_status pr2_token_sort_backward(const pr2_dims* dims, const void* dx, const int32_t* inv,
+                                   void* dh, void* stream);
+
+/* Expert rows back to token order, weighted: out[t] = sum_s gates[t, s] y[inv[t, s]] over the valid
+ * slots in slot order (Eq. pr2_output), fp32 sums rounded once.  y [T k, d], out [T, d] dtype;
+ * gates [T, k] fp32. */
+pr2_status pr2_token_unsort(const pr2_dims* dims, const void* y, const float* gates,
+                            const int32_t* inv, void* out, void* stream);
+
+/* Gradient of pr2_token_unsort: dy[inv[t, s]] = gates[t, s] dout[t] ([T k, d] dtype, zero past
+ * offsets[N]) and dgates[t, s] = <dout[t], y[inv[t, s]]> ([T, k] fp32, 0 for an invalid slot). */
+pr2_status pr2_token_unsort_backward(const pr2_dims* dims, const void* dout, const void* y,
+                                     const float* gates, const int32_t* inv,
+                                     const int32_t* offsets, void* dy, float* dgates,
+                                     void* stream);
+
+/*
+ * Gradient of the replay gates w.r.t. the router logits p = h W (gates of pr2_route_replay):
+ *     dlogits[t, j] = rho_j (sum_{s: idx_s = j} dgates[t, s] - sum_s dgates[t, s] rho_{idx_s}),
+ * and with PR2_F_NORMALIZE_TOPK, gates g_s = rho_{idx_s} / S, S = sum of the valid slots' rho:
+ *     dlogits[t, idx_s] = g_s (dgates[t, s] - sum_u dgates[t, u] g_u), 0 at the other experts.
+ *  probs [T, N] fp32 (pr2_route_replay's); idx [T, k]; dgates [T, k] fp32; dlogits [T, N] fp32
+ *  out.  An invalid slot (outside [0, N) or repeated) contributes nothing and sets
+ *  PR2_STATUS_BAD_INDEX; a token without a valid slot gets zeros.  T, N <= 256, k <= 32 and flags
+ *  of dims are used.
+ */
+pr2_status pr2_replay_gates_backward(const pr2_dims* dims, const float* probs, const int32_t* idx,
+                                     const float* dgates, float* dlogits, int32_t* status_dev,
+                                     void* stream);
+
+/* Elements of a row that share one scale in the 8-bit activation checkpoint. */
+#define PR2_CKPT_GROUP 128
+
+/* Rows of expert activations. */
+typedef struct {
+    int64_t rows;   /* e.g. T k rows in dispatch order                                          */
+    int64_t ld;     /* elements between rows of gate and up (and of dgate and dup), >= m: 2 m
+                     * for the two halves of one [rows, 2 m] matrix                             */
+    int32_t m;      /* expert hidden size, 1 <= m <= 2^24                                       */
+    int32_t dtype;  /* of every activation and gradient (pr2_dtype)                             */
+} pr2_act_dims;
+
+/*
+ * SwiGLU activation (App. E.2) that keeps its inputs in 8 bits for the backward pass:
+ *     act = silu(gate) * up,
+ * and for each run of PR2_CKPT_GROUP elements of a row of gate and of up (the last one may be
+ * shorter), with top = max |x| over the run:
+ *     scale = top / 127,  q = round(x 127 / top)  (to nearest, ties to even; x ~ q scale).
+ * The error of a held value is at most half a scale.  A run with top < 1e-30 is held as zeros; a
+ * run with an infinity or a NaN in it gets the scale NaN, so that its gradient is NaN too.
+ *  gate, up [rows, m] with row stride ld; act [rows, m] contiguous;
+ *  q [rows, 2, m] int8: a row's gate, then its up; scale [rows, 2, ceil(m / 128)] fp32.
+ */
+pr2_status pr2_swiglu_checkpoint(const pr2_act_dims* dims, const void* gate, const void* up,
+                                 void* act, int8_t* q, float* scale, void* stream);
+
+/*
+ * Its backward pass from the checkpoint, with g, u the held values and s = 1 / (1 + exp(-g)):
+ *     dgate = dact u s (1 + g (1 - s)),  dup = dact g s,  act = g s u (nullable: the activation
+ * again, for the gradient of the down projection).
+ *  dact [rows, m] contiguous; dgate, dup [rows, m] with row stride ld; act [rows, m] contiguous.
+ *  dgate, dup and act are buffers of their own, except that act may be dact.
+ */
+pr2_status pr2_swiglu_checkpoint_backward(const pr2_act_dims* dims, const void* dact,
+                                          const int8_t* q, const float* scale, void* dgate,
+                                          void* dup, void* act, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* pr2_strerror(pr2_status s);
 

@@ -28,6 +28,7 @@ PR2_F_NORMALIZE_TOPK = 0x4
 PR2_STATUS_BAD_INDEX = 0x1
 PR2_STATUS_TIMEOUT = 0x2
 PR2_NEAR_TIE_GAP = 1e-4
+PR2_CKPT_GROUP = 128
 STATUS_NAMES = {0: "PR2_OK", 1: "PR2_ERR_INVALID_ARG", 2: "PR2_ERR_UNSUPPORTED", 3: "PR2_ERR_CUDA",
                 4: "PR2_ERR_BAD_INDEX", 5: "PR2_ERR_TIMEOUT", 6: "PR2_ERR_WORKSPACE"}
 
@@ -63,6 +64,36 @@ def dims(T: int, d: int, N: int, k: int, m: int, n_shared: int = 0, dtype: str =
          flags: int = 0) -> Dims:
     code = {"fp32": PR2_FP32, "bf16": PR2_BF16}[dtype]
     return Dims(T, d, N, k, m, n_shared, code, flags)
+
+
+class PolicyDims(ctypes.Structure):
+    """``pr2_policy_dims``: T tokens, V vocabulary, row strides and the loss's constants."""
+
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld_logits", ctypes.c_int64),
+                ("ld_grad", ctypes.c_int64), ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+                ("inv_temp", ctypes.c_float), ("clip_low", ctypes.c_float),
+                ("clip_high", ctypes.c_float), ("kl_coef", ctypes.c_float),
+                ("grad_scale", ctypes.c_float)]
+
+
+def policy_dims(T: int, V: int, dtype: str = "bf16", ld_logits: Optional[int] = None,
+                ld_grad: Optional[int] = None, inv_temp: float = 1.0, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, grad_scale: float = 1.0,
+                flags: int = 0) -> PolicyDims:
+    code = {"fp32": PR2_FP32, "bf16": PR2_BF16}[dtype]
+    return PolicyDims(T, V, V if ld_logits is None else ld_logits, V if ld_grad is None else ld_grad,
+                      code, flags, inv_temp, clip_low, clip_high, kl_coef, grad_scale)
+
+
+class ActDims(ctypes.Structure):
+    """``pr2_act_dims``: rows of activations, their row stride, m = d_ff."""
+
+    _fields_ = [("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("m", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+def act_dims(rows: int, m: int, dtype: str = "bf16", ld: Optional[int] = None) -> ActDims:
+    return ActDims(rows, m if ld is None else ld, m, {"fp32": PR2_FP32, "bf16": PR2_BF16}[dtype])
 
 
 def library_path() -> str:
@@ -115,6 +146,20 @@ def load() -> ctypes.CDLL:
                                                 P, P, ctypes.c_size_t, P,
                                                 ctypes.POINTER(StageEvents), P]
         lib.pr2_moe_rollout_forward.restype = ctypes.c_int
+        PD, AD, SZ = ctypes.POINTER(PolicyDims), ctypes.POINTER(ActDims), ctypes.c_size_t
+        for name, res, args in (
+                ("pr2_policy_loss_workspace_bytes", SZ, [PD]),
+                ("pr2_policy_loss", ctypes.c_int, [PD] + [P] * 11 + [SZ, P, P]),
+                ("pr2_token_sort_workspace_bytes", SZ, [D]),
+                ("pr2_token_sort", ctypes.c_int, [D] + [P] * 7 + [SZ, P, P]),
+                ("pr2_token_sort_backward", ctypes.c_int, [D] + [P] * 4),
+                ("pr2_token_unsort", ctypes.c_int, [D] + [P] * 5),
+                ("pr2_token_unsort_backward", ctypes.c_int, [D] + [P] * 8),
+                ("pr2_replay_gates_backward", ctypes.c_int, [D] + [P] * 6),
+                ("pr2_swiglu_checkpoint", ctypes.c_int, [AD] + [P] * 6),
+                ("pr2_swiglu_checkpoint_backward", ctypes.c_int, [AD] + [P] * 7)):
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
         _lib = lib
         return lib
 
@@ -263,6 +308,70 @@ def pr2_rollout_layers(dm: Dims, L: int, h, W_router, W_pred, W_gate, W_up, W_do
                                      _p(status), _s(stream))
 
 
+# ---- training side -----------------------------------------------------------------------------
+
+def pr2_policy_loss_workspace_bytes(dm: PolicyDims) -> int:
+    return int(load().pr2_policy_loss_workspace_bytes(ctypes.byref(dm)))
+
+
+def pr2_policy_loss(dm: PolicyDims, logits, target, weight, advantage, logp_old, logp_ref, loss,
+                    logp=None, entropy=None, grad=None, workspace=None, ws_bytes=None, status=None,
+                    stream=None) -> int:
+    """Clipped policy loss with a KL term; ``grad`` (may be ``logits``) gets the gradient of the
+    logits.  ``loss`` [4]: total, policy part, KL part, weight of the clipped tokens."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return load().pr2_policy_loss(ctypes.byref(dm), _p(logits), _p(target), _p(weight),
+                                  _p(advantage), _p(logp_old), _p(logp_ref), _p(loss), _p(logp),
+                                  _p(entropy), _p(grad), _p(workspace), ws_bytes, _p(status),
+                                  _s(stream))
+
+
+def pr2_token_sort_workspace_bytes(dm: Dims) -> int:
+    return int(load().pr2_token_sort_workspace_bytes(ctypes.byref(dm)))
+
+
+def pr2_token_sort(dm: Dims, h, idx, x, offsets, perm, inv, workspace=None, ws_bytes=None,
+                   status=None, stream=None) -> int:
+    """Plan (offsets, perm, inv) of the route ``idx`` and the sorted rows ``x``; ``idx`` None: rows
+    by the plan given; ``h`` and ``x`` None: the plan alone."""
+    if ws_bytes is None:
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return load().pr2_token_sort(ctypes.byref(dm), _p(h), _p(idx), _p(x), _p(offsets), _p(perm),
+                                 _p(inv), _p(workspace), ws_bytes, _p(status), _s(stream))
+
+
+def pr2_token_sort_backward(dm: Dims, dx, inv, dh, stream=None) -> int:
+    return load().pr2_token_sort_backward(ctypes.byref(dm), _p(dx), _p(inv), _p(dh), _s(stream))
+
+
+def pr2_token_unsort(dm: Dims, y, gates, inv, out, stream=None) -> int:
+    return load().pr2_token_unsort(ctypes.byref(dm), _p(y), _p(gates), _p(inv), _p(out), _s(stream))
+
+
+def pr2_token_unsort_backward(dm: Dims, dout, y, gates, inv, offsets, dy, dgates,
+                              stream=None) -> int:
+    return load().pr2_token_unsort_backward(ctypes.byref(dm), _p(dout), _p(y), _p(gates), _p(inv),
+                                            _p(offsets), _p(dy), _p(dgates), _s(stream))
+
+
+def pr2_replay_gates_backward(dm: Dims, probs, idx, dgates, dlogits, status=None,
+                              stream=None) -> int:
+    return load().pr2_replay_gates_backward(ctypes.byref(dm), _p(probs), _p(idx), _p(dgates),
+                                            _p(dlogits), _p(status), _s(stream))
+
+
+def pr2_swiglu_checkpoint(dm: ActDims, gate, up, act, q, scale, stream=None) -> int:
+    return load().pr2_swiglu_checkpoint(ctypes.byref(dm), _p(gate), _p(up), _p(act), _p(q),
+                                        _p(scale), _s(stream))
+
+
+def pr2_swiglu_checkpoint_backward(dm: ActDims, dact, q, scale, dgate, dup, act=None,
+                                   stream=None) -> int:
+    return load().pr2_swiglu_checkpoint_backward(ctypes.byref(dm), _p(dact), _p(q), _p(scale),
+                                                 _p(dgate), _p(dup), _p(act), _s(stream))
+
+
 # ---- allocation helpers (plain torch.empty on the caller's device) ---------------------------
 
 def alloc_workspace(dm: Dims, device="cuda") -> torch.Tensor:
@@ -276,6 +385,20 @@ def alloc_loss_workspace(dm: Dims, device="cuda") -> torch.Tensor:
     n = pr2_predictor_loss_workspace_bytes(dm)
     if n == 0:
         raise Pr2Error(1, "pr2_predictor_loss_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_policy_workspace(dm: PolicyDims, device="cuda") -> torch.Tensor:
+    n = pr2_policy_loss_workspace_bytes(dm)
+    if n == 0:
+        raise Pr2Error(1, "pr2_policy_loss_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_token_workspace(dm: Dims, device="cuda") -> torch.Tensor:
+    n = pr2_token_sort_workspace_bytes(dm)
+    if n == 0:
+        raise Pr2Error(1, "pr2_token_sort_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 

@@ -49,12 +49,16 @@ bool make_tmap_bf16(CUtensorMap* m, const void* base, uint64_t inner, uint64_t o
   return r == CUDA_SUCCESS;
 }
 
+}  // namespace
+
 int num_sms_of_current_device() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 0;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
   return n;
 }
+
+namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -138,6 +142,8 @@ Workspace carve(const pr2_dims& dm, uint8_t* base) {
   return w;
 }
 
+}  // namespace
+
 pr2_status finish(cudaError_t err, uint32_t flags, int32_t* status_dev, cudaStream_t st) {
   if (err != cudaSuccess) return PR2_ERR_CUDA;
   if (flags & PR2_F_SYNC_STATUS) {
@@ -151,6 +157,8 @@ pr2_status finish(cudaError_t err, uint32_t flags, int32_t* status_dev, cudaStre
   }
   return PR2_OK;
 }
+
+namespace {
 
 // `slice`: aux is a later layer's part of a buffer whose start has been checked.  In fp32 it starts
 // at any float (T N need not be a multiple of 4), where the fp32 kernels store single floats; in

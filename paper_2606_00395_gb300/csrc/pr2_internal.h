@@ -222,6 +222,65 @@ cudaError_t launch_feature_cache(const void* h, const float* logits, int64_t T, 
                                  int d, int N, int esz, int32_t* pos, void* cache_h,
                                  float* cache_p, int num_sms, cudaStream_t st);
 
+// ---- host helpers (api.cu) -----------------------------------------------------------------
+int num_sms_of_current_device();  // 0 on error
+// The status of a call whose launches returned `err`; PR2_F_SYNC_STATUS waits and reads the word.
+pr2_status finish(cudaError_t err, uint32_t flags, int32_t* status_dev, cudaStream_t st);
+
+// ---- policy loss (policy_loss.cu) ----------------------------------------------------------
+struct PolicyArgs {
+  int64_t T, V, ld_logits, ld_grad;
+  int bf16;
+  float inv_temp, clip_low, clip_high, kl_coef, grad_scale;
+  const void* logits;
+  const int32_t* target;
+  const float *weight, *advantage, *logp_old, *logp_ref;  // nullable: weight, logp_old, logp_ref
+  float* loss;
+  float *logp, *entropy;  // nullable
+  void* grad;             // nullable; may be `logits`
+  double* partial;        // [kPolicyParts][4]
+  int32_t* status;        // nullable
+};
+constexpr int kPolicyParts = 4096;  // most groups of CTAs that sum tokens of their own
+cudaError_t launch_policy_loss(const PolicyArgs& a, int num_sms, cudaStream_t st);
+
+// ---- tokens sorted by expert, and back (token_sort.cu) -------------------------------------
+struct TokenArgs {
+  int64_t T;
+  int d, N, k, bf16;
+  const int32_t* inv;      // [T k]
+  const int32_t* offsets;  // [N + 1] (sort and unsort_backward)
+  int32_t* perm;           // [T k], its tail is filled (nullable; sort)
+  const float* gates;      // [T k] (unsort, unsort_backward)
+  const void* src;         // sort: h; sort_backward: dx; unsort: y; unsort_backward: dout
+  const void* y;           // unsort_backward
+  void* dst;               // sort: x; sort_backward: dh; unsort: out; unsort_backward: dy
+  float* dgates;           // unsort_backward
+  const int32_t* status;   // sort: of the dispatch before it (nullable)
+};
+cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_token_sum(const TokenArgs& a, int num_sms, cudaStream_t st);  // gates nullable
+cudaError_t launch_token_unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st);
+
+// ---- gradient of the replay gates (gates_grad.cu) -------------------------------------------
+cudaError_t launch_gates_backward(const float* probs, const int32_t* idx, const float* dgates,
+                                  int64_t T, int N, int k, bool norm, float* dlogits,
+                                  int32_t* status, int num_sms, cudaStream_t st);
+
+// ---- 8-bit activation checkpoint (act_checkpoint.cu) ----------------------------------------
+struct ActArgs {
+  int64_t rows, ld;
+  int m, bf16;
+  const void *gate, *up;  // forward
+  const void* dact;       // backward
+  int8_t* q;
+  float* scale;
+  void* act;              // nullable in the backward pass
+  void *dgate, *dup;
+};
+cudaError_t launch_swiglu_checkpoint(const ActArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_swiglu_backward(const ActArgs& a, int num_sms, cudaStream_t st);
+
 // ---- self test (api.cu) --------------------------------------------------------------------
 cudaError_t launch_wait_selftest(int32_t* status, int64_t timeout_ns, cudaStream_t st);
 

@@ -1,0 +1,279 @@
+"""GPU policy loss (pr2_policy_loss) against the plain 64-bit form.
+
+Tolerances.  z = inv_temp logit is rounded once (2^-24 |z|, |z| < 40 here: 2.4e-6) and the
+exponentials are good to a few 2^-22, sums of positive terms add no more than a few roundings in the
+depth of their tree, so l has a relative error below 1e-5 and logp an absolute one below 1e-5 plus
+the rounding of logp itself (2^-24 |logp|).  The entropy weights |x| < 40 with those errors: 1e-4.
+A gradient entry is f ([v = a] - p): p's relative error 1e-5 and f's (through the ratio and the KL
+factor) both scale with the row's terms (`scale` of the reference): 3e-5 of it, plus one rounding of
+the stored type.  loss is a sum of terms with relative errors 2e-5 of their size.
+"""
+import math
+
+import pytest
+import torch
+
+import train_reference as R
+from paper_2606_00395_gb300 import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+EPS = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -23}
+
+
+def make(T, V, dtype, seed, pad=0, banned=0.0, shift=0, std=2.0):
+    g = torch.Generator().manual_seed(seed)
+    ld = V + pad
+    buf = torch.empty(T * ld + shift + 64, dtype=DT[dtype])
+    logits = buf[shift:shift + T * ld].view(T, ld)
+    z = std * torch.randn(T, ld, generator=g)
+    target = torch.randint(0, V, (T,), generator=g).int()
+    if banned:
+        z[torch.rand(T, ld, generator=g) < banned] = -math.inf
+    z[torch.arange(T), target.long()] = 6 * torch.rand(T, generator=g)
+    z[:, V:] = 1e4  # padding columns hold anything
+    logits.copy_(z)
+    lp = torch.log_softmax(logits[:, :V].double(), 1)[torch.arange(T), target.long()]
+    # ratios stay clear of the clip bounds, where a last bit decides
+    drift = torch.tensor([0.05, -0.1, 0.4, -0.5, 0.15])[torch.randint(0, 5, (T,), generator=g)]
+    weight = torch.where(torch.rand(T, generator=g) < 0.25, 0.0, torch.rand(T, generator=g) / T + 1e-3)
+    return dict(buf=buf, shift=shift, ld=ld, V=V, logits=logits, target=target, weight=weight,
+                advantage=torch.randn(T, generator=g), logp_old=(lp - drift).float(),
+                logp_ref=(lp + 0.3 * torch.randn(T, generator=g, dtype=torch.float64)).float())
+
+
+def call(c, dtype, names=("weight", "logp_old", "logp_ref"), grad=True, inplace=False, ld_grad=None,
+         **kw):
+    T, V, ld = c["logits"].shape[0], c["V"], c["ld"]
+    dev = c["buf"].cuda()
+    logits = dev[c["shift"]:c["shift"] + T * ld].view(T, ld)
+    opt = {n: c[n].cuda() if n in names else None for n in ("weight", "logp_old", "logp_ref")}
+    ldg = ld if ld_grad is None else ld_grad
+    dm = B.policy_dims(T, V, dtype, ld_logits=ld, ld_grad=ldg, **kw)
+    loss = torch.full((4,), math.nan, device="cuda")
+    logp, ent = (torch.full((T,), math.nan, device="cuda") for _ in range(2))
+    out = logits if inplace else torch.full((T, ldg), 7.0, dtype=DT[dtype], device="cuda") if grad else None
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.check(B.pr2_policy_loss(dm, logits, c["target"].cuda(), opt["weight"], c["advantage"].cuda(),
+                              opt["logp_old"], opt["logp_ref"], loss, logp, ent, out,
+                              B.alloc_policy_workspace(dm), status=status), "pr2_policy_loss")
+    torch.cuda.synchronize()
+    return dict(loss=loss.cpu(), logp=logp.cpu(), entropy=ent.cpu(), status=int(status.item()),
+                grad=None if out is None else out.cpu())
+
+
+def check(c, got, dtype, names=("weight", "logp_old", "logp_ref"), **kw):
+    ref = R.policy(c["logits"][:, :c["V"]], c["target"], c["advantage"],
+                   **{n: c[n] for n in names}, **kw)
+    assert torch.isfinite(ref["loss"]).all()
+    live = torch.isfinite(ref["logp"])
+    assert torch.equal(got["logp"][~live].double(), ref["logp"][~live])
+    err = (got["logp"].double() - ref["logp"])[live].abs()
+    assert (err <= 1e-5 + 2.0 ** -24 * ref["logp"][live].abs()).all(), float(err.max())
+    assert ((got["entropy"].double() - ref["entropy"]).abs() <= 1e-4).all()
+    size = float((ref["scale"].sum() + ref["loss"].abs().sum()))
+    assert ((got["loss"].double() - ref["loss"]).abs() <= 2e-5 * size).all()
+    if got["grad"] is not None:
+        g = got["grad"][:, :c["V"]].double()
+        bound = 3e-5 * ref["scale"][:, None] + EPS[dtype] * ref["grad"].abs()
+        assert ((g - ref["grad"]).abs() <= bound).all()
+    return ref
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,V,pad,shift", [
+    (1, 1, 0, 0), (1, 2, 0, 1), (3, 7, 1, 0), (5, 33, 0, 3), (4, 255, 0, 1), (7, 1000, 24, 0),
+    (2, 4097, 0, 5), (9, 8192, 0, 0), (300, 515, 0, 0), (700, 64, 0, 0), (3, 32001, 0, 0),
+    (1, 70003, 0, 0), (2, 131072, 8, 8), (1, 300001, 0, 1)])
+def test_loss_and_gradient(dtype, T, V, pad, shift):
+    c = make(T, V, dtype, T * 31 + V, pad=pad, shift=shift)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05)
+    got = call(c, dtype, **kw)
+    check(c, got, dtype, **kw)
+    assert got["status"] == 0
+    if pad:
+        assert (got["grad"][:, V:] == 7.0).all()  # the padding columns are left alone
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_rows_a_block(dtype):
+    c = make(3001, 130, dtype, 4)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05, inv_temp=1.25, grad_scale=3.0)
+    check(c, call(c, dtype, **kw), dtype, **kw)
+
+
+@pytest.mark.parametrize("V,ld_grad", [(1000, 1001), (1024, 1040), (333, 334)])
+def test_gradient_rows_of_another_stride(V, ld_grad):
+    c = make(6, V, "bf16", V)
+    got = call(c, "bf16", ld_grad=ld_grad)
+    check(c, got, "bf16", clip_low=0.2, clip_high=0.2)
+    assert (got["grad"][:, V:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,V,pad", [("bf16", 1024, 0), ("bf16", 40001, 0), ("fp32", 777, 3)])
+def test_gradient_in_place_of_the_logits(dtype, V, pad):
+    c = make(37, V, dtype, 11, pad=pad)
+    kw = dict(clip_high=0.28, kl_coef=0.1)
+    apart, same = call(c, dtype, **kw), call(c, dtype, inplace=True, **kw)
+    for n in ("loss", "logp", "entropy"):
+        assert torch.equal(apart[n], same[n])
+    assert torch.equal(apart["grad"][:, :V], same["grad"][:, :V])
+
+
+def test_optional_inputs_and_outputs():
+    c = make(50, 300, "fp32", 2)
+    got = call(c, "fp32", names=(), grad=False)
+    check(c, got, "fp32", names=())
+    assert float(got["loss"][2]) == 0.0 and got["grad"] is None
+    check(c, call(c, "fp32", names=("logp_ref",), kl_coef=0.2), "fp32", names=("logp_ref",), kl_coef=0.2)
+    # the KL part is measured even where it has no weight in the loss
+    seen = call(c, "fp32", names=("logp_ref",))
+    check(c, seen, "fp32", names=("logp_ref",))
+    assert float(seen["loss"][0]) == float(seen["loss"][1]) and float(seen["loss"][2]) > 0
+    dm = B.policy_dims(50, 300, "fp32")
+    loss = torch.empty(4, device="cuda")
+    B.check(B.pr2_policy_loss(dm, c["logits"].cuda(), c["target"].cuda(), None, c["advantage"].cuda(),
+                              None, None, loss, None, None, None, B.alloc_policy_workspace(dm)))
+    assert torch.equal(loss.cpu(), got["loss"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_banned_entries_and_empty_rows(dtype):
+    c = make(12, 3000, dtype, 8, banned=0.4)
+    c["logits"][3] = -math.inf           # nothing can be sampled
+    c["logits"][4] = torch.finfo(DT[dtype]).min  # the type's lowest value everywhere: uniform
+    c["logits"][5, :] = -math.inf
+    c["logits"][5, c["target"][5].long()] = 1.0  # one token left: p = 1
+    c["weight"][:6] = 0.01
+    c["logp_old"][4:6] = 0.0
+    c["logp_ref"][4:6] = -0.1
+    c["logp_old"][4] = c["logp_ref"][4] = -math.log(3000)
+    kw = dict(clip_high=0.28, kl_coef=0.05)
+    got = call(c, dtype, **kw)
+    check(c, got, dtype, **kw)
+    assert got["logp"][3] == -math.inf and got["entropy"][3] == 0 and not got["grad"][3].any()
+    assert not got["grad"][c["logits"] == -math.inf].any()
+
+
+def test_tokens_that_do_not_count_are_not_read():
+    c = make(20, 500, "bf16", 9)
+    kw = dict(kl_coef=0.05)
+    c["weight"][:] = 0.02
+    c["weight"][7] = c["weight"][13] = c["weight"][19] = 0.0
+    want = call(c, "bf16", **kw)
+    for t, bad in ((7, math.nan), (13, math.inf), (19, math.nan)):
+        c["logits"][t] = bad
+        c["advantage"][t] = c["logp_old"][t] = c["logp_ref"][t] = bad
+    c["target"][7] = -100
+    got = call(c, "bf16", **kw)
+    for n in ("loss", "logp", "entropy", "grad"):
+        assert torch.equal(got[n], want[n]), n
+    assert got["status"] == 0 and not got["grad"][7].any() and got["logp"][7] == 0
+
+
+def test_targets_out_of_range_are_flagged_and_left_out():
+    c = make(20, 500, "fp32", 10)
+    c["weight"][:] = 0.05
+    good = dict(c, weight=c["weight"].clone(), target=c["target"].clone())
+    good["weight"][4] = good["weight"][9] = 0.0
+    c["target"][4], c["target"][9] = 500, -1
+    a, b = call(c, "fp32"), call(good, "fp32")
+    assert a["status"] == B.PR2_STATUS_BAD_INDEX and b["status"] == 0
+    for n in ("loss", "logp", "entropy", "grad"):
+        assert torch.equal(a[n], b[n]), n
+
+
+def test_extremes():
+    c = make(8, 200, "fp32", 12)
+    c["weight"][:] = 0.125
+    c["advantage"][:] = torch.tensor([0.0, 0.0, -1.0, 1.0, 1.0, 1.0, 1.0, 1.0])
+    c["logp_old"][0] = -1000.0   # ratio overflows; the advantage is 0
+    c["logits"][3] += 80.0       # a large offset changes nothing
+    got = call(c, "fp32", names=("weight", "logp_old"))
+    assert torch.isfinite(got["loss"]).all() and torch.isfinite(got["grad"]).all()
+    assert not got["grad"][0].any()
+    for bad in (math.nan, math.inf):  # a row that holds one is loud
+        d = dict(c, logits=None)
+        d["buf"] = c["buf"].clone()
+        d["logits"] = d["buf"][:8 * 200].view(8, 200)
+        d["logits"][5, 17] = bad
+        got = call(d, "fp32", names=("weight", "logp_old"))
+        assert torch.isnan(got["logp"][5]) and torch.isnan(got["loss"][0]) and torch.isnan(got["grad"][5]).all()
+        assert torch.isfinite(got["logp"][[0, 1, 2, 3, 4, 6, 7]]).all()
+
+
+@pytest.mark.parametrize("T,V", [(64, 5000), (2000, 999)])
+def test_same_bits_twice_and_on_another_stream(T, V):
+    c = make(T, V, "bf16", 13)
+    a = call(c, "bf16", kl_coef=0.05)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        b = call(c, "bf16", kl_coef=0.05)
+    for n in ("loss", "logp", "entropy", "grad"):
+        assert torch.equal(a[n], b[n]), n
+
+
+def test_captured_in_a_graph():
+    c = make(40, 2000, "bf16", 14)
+    want = call(c, "bf16", kl_coef=0.05)
+    dm = B.policy_dims(40, 2000, "bf16", kl_coef=0.05)
+    t = {n: c[n].cuda() for n in ("logits", "target", "weight", "advantage", "logp_old", "logp_ref")}
+    loss, grad, ws = torch.zeros(4, device="cuda"), torch.zeros_like(t["logits"]), B.alloc_policy_workspace(dm)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.check(B.pr2_policy_loss(dm, t["logits"], t["target"], t["weight"], t["advantage"], t["logp_old"],
+                                  t["logp_ref"], loss, None, None, grad, ws))
+    for _ in range(2):
+        loss.zero_()
+        grad.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss.cpu(), want["loss"]) and torch.equal(grad.cpu(), want["grad"])
+
+
+def test_gradient_against_differences_of_the_loss():
+    """fp32 differences: loss errors 2e-5 of the terms' size over a step of 2^-6 give 3e-3 of it, the
+    step's own error is below 2^-12 of it."""
+    c = make(4, 50, "fp32", 21, std=1.0)
+    c["weight"][:] = 0.25
+    kw = dict(clip_high=0.28, kl_coef=0.1)
+    base = call(c, "fp32", **kw)
+    size = float(R.policy(c["logits"], c["target"], c["advantage"], weight=c["weight"], logp_old=c["logp_old"],
+                          logp_ref=c["logp_ref"], **kw)["scale"].max())
+    h = 2.0 ** -6
+    for t in range(4):
+        for v in (int(c["target"][t]), 3, 49):
+            two = []
+            for sign in (1, -1):
+                keep = c["logits"][t, v].clone()
+                c["logits"][t, v] += sign * h
+                two.append(float(call(c, "fp32", grad=False, **kw)["loss"][0]))
+                c["logits"][t, v] = keep
+            assert abs((two[0] - two[1]) / (2 * h) - float(base["grad"][t, v])) <= 4e-3 * size
+
+
+def test_empty_batch_writes_zero_loss():
+    dm = B.policy_dims(0, 100, "bf16")
+    loss = torch.ones(4, device="cuda")
+    B.check(B.pr2_policy_loss(dm, None, None, None, None, None, None, loss))
+    assert not loss.cpu().any()
+
+
+def test_rows_beyond_32_bit_offsets():
+    T, V = 18000, 131072  # 2.36e9 logits; only a few rows count
+    dm = B.policy_dims(T, V, "bf16")
+    logits = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(T, device="cuda")
+    rows = torch.tensor([0, 16384, 17999])
+    w[rows.cuda()] = 0.5
+    target = torch.full((T,), V - 1, dtype=torch.int32, device="cuda")
+    logits[rows.cuda(), V - 1] = 10.0
+    loss, logp = torch.empty(4, device="cuda"), torch.empty(T, device="cuda")
+    B.check(B.pr2_policy_loss(dm, logits, target, w, torch.ones(T, device="cuda"), None, None, loss, logp, None,
+                              logits, B.alloc_policy_workspace(dm)))
+    p = math.exp(10) / (math.exp(10) + V - 1)
+    assert torch.allclose(logp[rows.cuda()].cpu().double(), torch.full((3,), math.log(p), dtype=torch.float64), atol=1e-5)
+    got = logits[rows.cuda()].cpu().double()
+    assert torch.allclose(got[:, V - 1], torch.full((3,), -0.5 * (1 - p), dtype=torch.float64), rtol=2.0 ** -8)
+    assert torch.allclose(got[:, 0], torch.full((3,), 0.5 * (1 - p) / (V - 1), dtype=torch.float64), rtol=2.0 ** -8)
+    assert not logits[1].any()
