@@ -12,10 +12,12 @@
 // difference first, which is exact or nearly so and cannot overflow where a scaled logit could (a
 // row at the type's lowest value).
 //
-// A row is read from HBM once: the CTAs of a cluster split it and each keeps its slice in shared
-// memory (bulk copies, the next row's slice in flight) between the two passes; they exchange their
-// three sums through distributed shared memory.  Short rows go to one warp each, and rows that no
-// cluster's shared memory holds are read twice.
+// A row is read from HBM once.  A producer warp streams it, by bulk copies, through a ring of chunks
+// in shared memory, and the chunks that fit stay there between the passes.  Of a longer row the first
+// chunks are let go after the first pass and come again, from L2, after the others in the second; in
+// the order of loading and of release the ring is first in, first out throughout.  The slots that the
+// second pass frees take the next row's chunks.  The CTAs of a cluster may split a row: they exchange
+// their three sums through distributed shared memory.  Short rows go to one warp each.
 // Tokens are dealt to clusters (warps) by their number; each sums its tokens' terms in double and
 // policy_finish_kernel the clusters' in order, so the loss does not depend on timing.
 #include <math_constants.h>
@@ -153,7 +155,6 @@ __device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / V
   const float ref = s.m == -CUDART_INF_F ? 0.f : -s.m;
   const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(ref, ref);
   uint64_t l2 = 0, e2 = 0;
-  float y[16];
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
     uint64_t z[kPairs];
@@ -166,8 +167,6 @@ __device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / V
       const uint64_t p2 = pack2(exp2_approx(a), exp2_approx(b));
       l2 = add2(l2, p2);
       e2 = fma2(p2, x2, e2);
-      y[(j * kPairs + i) * 2] = a;
-      y[(j * kPairs + i) * 2 + 1] = b;
     }
   }
   float a, b;
@@ -178,8 +177,16 @@ __device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / V
   if (e != e) {
     e = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (y[i] != -CUDART_INF_F) e = fmaf(exp2_approx(y[i]), y[i], e);
+    for (int j = 0; j < kVecs; ++j) {
+      uint64_t z[kPairs];
+      Vec<T>::pairs(raw[j], z);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        unpack2(mul2(add2(z[i], ref2), scale2), a, b);
+        if (a != -CUDART_INF_F) e = fmaf(exp2_approx(a), a, e);
+        if (b != -CUDART_INF_F) e = fmaf(exp2_approx(b), b, e);
+      }
+    }
   }
   s.e += e;
 }
@@ -187,30 +194,29 @@ __device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / V
 // Where a row lies: `head` entries before its first 16-byte boundary, nvec whole vectors, then
 // `tail` entries.
 struct RowShape {
-  int head, tail;
-  int64_t nvec;
+  int head, tail, nvec;
 };
 template <typename T>
-__device__ __forceinline__ RowShape row_shape(const T* row, int64_t V) {
+__device__ __forceinline__ RowShape row_shape(const T* row, int V) {
   constexpr int E = Vec<T>::kElems;
   const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
   RowShape s;
   s.head = off != 0 ? E - off : 0;
-  if (s.head > V) s.head = static_cast<int>(V);
+  if (s.head > V) s.head = V;
   s.nvec = (V - s.head) / E;
-  s.tail = static_cast<int>(V - s.head - s.nvec * E);
+  s.tail = V - s.head - s.nvec * E;
   return s;
 }
 
 // Sums over vectors src[0 .. n), thread `tid` of kStride taking each kStride-th.
 template <typename T, int kStride>
-__device__ __forceinline__ void sum_span(RowSum& s, const uint4* src, int64_t n, int tid, float scale) {
+__device__ __forceinline__ void sum_span(RowSum& s, const uint4* src, int n, int tid, float scale) {
   constexpr int kVecs = 16 / Vec<T>::kElems;
-  for (int64_t base = 0; base < n; base += kStride * kVecs) {
+  for (int base = 0; base < n; base += kStride * kVecs) {
     uint4 raw[kVecs];
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-      const int64_t v = base + j * kStride + tid;
+      const int v = base + j * kStride + tid;
       raw[j] = v < n ? src[v]
                      : make_uint4(Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf);
     }
@@ -231,23 +237,23 @@ __device__ __forceinline__ T grad_one(float z, const RowGrad& g, float scale, bo
 // Gradient of vectors src[0 .. n) to out (entry `first` of the row on; 16-byte aligned or not).
 // f = 0 writes zeros and reads nothing.  `at`: the target's entry relative to src, or outside.
 template <typename T, int kStride>
-__device__ __forceinline__ void grad_span(const uint4* src, T* out, int64_t n, int tid, const RowGrad& g,
-                                          float scale, int64_t at) {
+__device__ __forceinline__ void grad_span(const uint4* src, T* out, int n, int tid, const RowGrad& g,
+                                          float scale, int at) {
   constexpr int E = Vec<T>::kElems, kPairs = E / 2;
   if ((reinterpret_cast<uintptr_t>(out) & 15u) != 0) {  // rows of another alignment than the logits'
     const T* one = reinterpret_cast<const T*>(src);
-    for (int64_t i = tid; i < n * E; i += kStride)
+    for (int i = tid; i < n * E; i += kStride)
       out[i] = g.f != 0.f ? grad_one<T>(to_f32<T>(one[i]), g, scale, i == at) : from_f32<T>(0.f);
     return;
   }
   uint4* dst = reinterpret_cast<uint4*>(out);
   if (g.f == 0.f) {
-    for (int64_t v = tid; v < n; v += kStride) __stcs(dst + v, make_uint4(0u, 0u, 0u, 0u));
+    for (int v = tid; v < n; v += kStride) __stcs(dst + v, make_uint4(0u, 0u, 0u, 0u));
     return;
   }
   const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-g.m, -g.m), fl2 = pack2(-g.fl, -g.fl);
 #pragma unroll 2
-  for (int64_t v = tid; v < n; v += kStride) {
+  for (int v = tid; v < n; v += kStride) {
     uint64_t z[kPairs];
     Vec<T>::pairs(src[v], z);
 #pragma unroll
@@ -278,11 +284,11 @@ __device__ __forceinline__ RowSum join_warp(RowSum s, float scale) {
 
 // ---- a token ------------------------------------------------------------------------------------
 struct Token {
-  int64_t t;
+  int t;
   float w;  // 0: does not count (or beyond the batch)
   int target;
 };
-__device__ __forceinline__ Token load_token(const PolicyArgs& a, int64_t t, bool flag) {
+__device__ __forceinline__ Token load_token(const PolicyArgs& a, int t, bool flag) {
   Token k{t, 0.f, 0};
   if (t >= a.T) return k;
   k.w = a.weight != nullptr ? a.weight[t] : 1.f / static_cast<float>(a.T);
@@ -305,7 +311,7 @@ __device__ __forceinline__ TokenIn load_inputs(const PolicyArgs& a, const Token&
   in.A = a.advantage[k.t];
   if (a.logp_old != nullptr) in.old = a.logp_old[k.t];
   if (a.logp_ref != nullptr) in.ref = a.logp_ref[k.t];
-  in.za = to_f32<T>(static_cast<const T*>(a.logits)[k.t * a.ld_logits + k.target]);
+  in.za = to_f32<T>(static_cast<const T*>(a.logits)[static_cast<int64_t>(k.t) * a.ld_logits + k.target]);
   return in;
 }
 
@@ -355,17 +361,74 @@ __device__ __forceinline__ void write_loss(const PolicyArgs& a, const double (&s
   for (int j = 0; j < 3; ++j) a.loss[1 + j] = static_cast<float>(s[j]);
 }
 
-// ---- rows split over a cluster -------------------------------------------------------------------
-// `cap` vectors a CTA at most; kResident: they stay in shared memory (`slots` buffers, one row each),
-// else both passes read them from global memory.
-template <typename T, bool kResident>
-__global__ void __launch_bounds__(kThreads)
-    policy_cluster_kernel(const PolicyArgs a, int C, int64_t cap, int slots) {
-  extern __shared__ uint4 data[];
-  __shared__ RowSum part[kWarps];
+// ---- rows through a ring of chunks -----------------------------------------------------------------
+constexpr int kRing = 4;             // chunks of a CTA's ring
+constexpr int kChunkVecs = 1024;     // 16-byte vectors of a chunk
+constexpr int kChunkBytes = kChunkVecs * 16;
+constexpr int kRowThreads = kThreads + 32;  // eight consumer warps, one producer
+constexpr int kBarConsumers = 1;
+
+// A place in the ring: slot and how often the ring went round (its parity).
+struct RingAt {
+  int slot;
+  uint32_t round;
+  __device__ __forceinline__ void step() {
+    if (++slot == kRing) {
+      slot = 0;
+      round ^= 1u;
+    }
+  }
+};
+
+__device__ __forceinline__ void arrive_cluster(uint64_t* bar, uint32_t rank) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                   mapa_shared(smem_u32(bar), rank))
+               : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Bounded, as mbar_wait.
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                             int32_t* status) {
+  if (try_wait_cluster(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (try_wait_cluster(bar, parity)) return true;
+    if ((it & 63u) == 0u) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        if (status != nullptr) atomicOr(status, PR2_STATUS_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
+// A CTA's part of a row: `n` vectors from vector v0 on, in `chunks` chunks.
+struct Slice {
+  RowShape sh;
+  int n, chunks;
+};
+
+// C CTAs a row, `cap` vectors each at most.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, 3)
+    policy_row_kernel(const PolicyArgs a, int C, int cap) {
+  extern __shared__ uint4 ring[];
+  __shared__ RowSum part[2][kWarps];
   __shared__ float4 xchg[2][kMaxCluster];
   __shared__ RowGrad row_grad;
-  __shared__ uint64_t full[2];
+  __shared__ uint64_t full[kRing], empty[kRing], met[2];
   __shared__ int abort_flag_s;
   volatile int* abort_flag = &abort_flag_s;
   constexpr int E = Vec<T>::kElems;
@@ -373,132 +436,182 @@ __global__ void __launch_bounds__(kThreads)
   const int rank = C > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   if (tid == 0) {
     abort_flag_s = 0;
-    mbar_init(&full[0], 1);
-    mbar_init(&full[1], 1);
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], kWarps);
+    }
+    mbar_init(&met[0], C);
+    mbar_init(&met[1], C);
     fence_mbar_init();
   }
   if (C > 1)
-    cluster_sync();  // peers write here from the first row on
+    cluster_sync();  // peers arrive here from the first row on
   else
     __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const float scale = a.inv_temp * kLog2e;
   const T* logits = static_cast<const T*>(a.logits);
-  T* grad = static_cast<T*>(a.grad);
-  const int64_t groups = gridDim.x / C, first = blockIdx.x / C;
-  const int64_t v0 = rank * cap;
-  auto span = [&](const RowShape& sh) {
-    const int64_t left = sh.nvec - v0;
-    return left < 0 ? int64_t{0} : left < cap ? left : cap;
+  const bool hold = a.grad != nullptr;
+  const int groups = static_cast<int>(gridDim.x) / C, first = static_cast<int>(blockIdx.x) / C;
+  const int v0 = rank * cap;
+  auto row_of = [&](int t) { return logits + t * a.ld_logits; };
+  auto slice_of = [&](int t) {
+    Slice s;
+    s.sh = row_shape(row_of(t), static_cast<int>(a.V));
+    const int left = s.sh.nvec - v0;
+    s.n = left < 0 ? 0 : left < cap ? left : cap;
+    s.chunks = static_cast<int>((s.n + kChunkVecs - 1) / kChunkVecs);
+    return s;
   };
-  int issued[2] = {0, 0};
-  auto issue = [&](const Token& k, int slot) {  // by thread 0
-    if (k.w == 0.f) return;
-    const T* row = logits + k.t * a.ld_logits;
-    const RowShape sh = row_shape(row, a.V);
-    const int64_t n = span(sh);
-    if (n == 0) return;
-    const char* src = reinterpret_cast<const char*>(row + sh.head) + v0 * 16;
-    ++issued[slot];
-    mbar_arrive_expect_tx(&full[slot], static_cast<uint32_t>(n * 16));
-    constexpr int64_t kPiece = 8192;
-    for (int64_t at = 0; at < n * 16; at += kPiece) {
-      const int64_t left = n * 16 - at;
-      bulk_load(smem_u32(data + slot * cap) + static_cast<uint32_t>(at), src + at,
-                static_cast<uint32_t>(left < kPiece ? left : kPiece), &full[slot]);
-    }
-  };
-  Token cur = load_token(a, first, rank == 0 && tid == 0);
-  Token next = load_token(a, first + groups, rank == 0 && tid == 0);
-  if (kResident && tid == 0) {
-    issue(cur, 0);
-    if (slots == 2) issue(next, 1);
-  }
-  uint32_t phases = 0;
-  double sums[3] = {0.0, 0.0, 0.0};
-  int parity = 0, slot = 0;
-  for (; cur.t < a.T;) {
-    const Token after = load_token(a, cur.t + 2 * groups, rank == 0 && tid == 0);
-    const T* row = logits + cur.t * a.ld_logits;
-    const RowShape sh = row_shape(row, a.V);
-    const int64_t n = span(sh);
-    const uint4* src = kResident ? data + slot * cap
-                                 : reinterpret_cast<const uint4*>(row + sh.head) + v0;
-    // the entries outside whole vectors: threads 0-7 the head's, 8-15 the tail's, of rank 0
-    int64_t edge = -1;
-    if (rank == 0 && tid < 16) {
-      if (tid < 8 && tid < sh.head) edge = tid;
-      if (tid >= 8 && tid - 8 < sh.tail) edge = a.V - sh.tail + (tid - 8);
-    }
-    float ez = 0.f;
-    RowGrad g{0.f, 0.f, 0.f, 0.f};
-    if (cur.w != 0.f) {
-      RowSum s{-CUDART_INF_F, 0.f, 0.f};
-      if (edge >= 0) {
-        ez = to_f32<T>(row[edge]);
-        add_one(s, ez, scale);
-      }
-      TokenIn in{};
-      if (warp == 0) in = load_inputs<T>(a, cur);
-      if (kResident && n > 0) {
-        mbar_wait(&full[slot], (phases >> slot) & 1u, abort_flag, a.status);
-        phases ^= 1u << slot;
-      }
-      sum_span<T, kThreads>(s, src, n, tid, scale);
-      s = join_warp(s, scale);
-      if (lane == 0) part[warp] = s;
-      __syncthreads();
-      if (warp == 0) {
-        s = lane < kWarps ? part[lane] : RowSum{-CUDART_INF_F, 0.f, 0.f};
-        s = join_warp(s, scale);
-        if (C > 1 && lane < C)
-          st_cluster_v4(mapa_shared(smem_u32(&xchg[parity][rank]), lane), __float_as_uint(s.m),
-                        __float_as_uint(s.l), __float_as_uint(s.e), 0u);
-      }
-      if (C > 1) cluster_sync();
-      // (a peer that is a row ahead writes the other half of xchg, and none is two ahead)
-      if (warp == 0) {
-        if (C > 1) {
-          const float4 x = lane < C ? xchg[parity][lane] : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
-          s = join_warp(RowSum{x.x, x.y, x.z}, scale);
+
+  if (warp == kWarps) {
+    // ---------------- producer ----------------
+    if (lane == 0) {
+      RingAt at{0, 0u};
+      uint32_t landing = 0, last_round = 0;  // slots with a copy issued, and its round
+      Token cur = load_token(a, first, false);
+      bool ok = true;
+      while (cur.t < a.T && ok) {
+        const Token next = load_token(a, cur.t + groups, false);
+        if (cur.w != 0.f) {
+          const Slice s = slice_of(cur.t);
+          const char* src = reinterpret_cast<const char*>(row_of(cur.t) + s.sh.head) + static_cast<int64_t>(v0) * 16;
+          const int again = hold && s.chunks > kRing ? s.chunks - kRing : 0;
+          for (int i = 0; i < s.chunks + again && ok; ++i) {
+            const int v = (i < s.chunks ? i : i - s.chunks) * kChunkVecs;
+            const int left = s.n - v;
+            const uint32_t bytes = static_cast<uint32_t>(left < kChunkVecs ? left : kChunkVecs) * 16u;
+            ok = mbar_wait(&empty[at.slot], at.round ^ 1u, abort_flag, a.status);
+            if (!ok) break;
+            mbar_arrive_expect_tx(&full[at.slot], bytes);
+            bulk_load(smem_u32(ring + at.slot * kChunkVecs), src + static_cast<int64_t>(v) * 16, bytes, &full[at.slot]);
+            landing |= 1u << at.slot;
+            last_round = (last_round & ~(1u << at.slot)) | (at.round << at.slot);
+            at.step();
+          }
         }
-        g = finish_token(a, cur, in, s, rank == 0 && lane == 0, sums);
-        if (lane == 0) row_grad = g;
+        cur = next;
       }
-      __syncthreads();
-      g = row_grad;
-      parity ^= 1;
-    } else if (rank == 0 && tid == 0) {
-      if (a.logp != nullptr) a.logp[cur.t] = 0.f;
-      if (a.entropy != nullptr) a.entropy[cur.t] = 0.f;
+      // no copy may still be landing when the CTA leaves (the consumers may have given up)
+      for (int i = 0; i < kRing; ++i)
+        if ((landing >> i) & 1u)
+          mbar_wait_slow(&full[i], (last_round >> i) & 1u, nullptr, nullptr, kDrainLimitNs);
     }
-    if (grad != nullptr) {
-      T* out = grad + cur.t * a.ld_grad;
-      const int64_t start = sh.head + v0 * E;
-      grad_span<T, kThreads>(src, out + start, n, tid, g, scale, cur.target - start);
-      if (edge >= 0)
-        out[edge] = g.f != 0.f ? grad_one<T>(ez, g, scale, edge == cur.target) : from_f32<T>(0.f);
+  } else {
+    // ---------------- consumers ----------------
+    // (after a wait ran out, ok is false: the warp waits for no copy any more and skips the work, but
+    // goes the same way through the barriers that the others may be waiting at)
+    const float scale = a.inv_temp * kLog2e;
+    T* grad = static_cast<T*>(a.grad);
+    RingAt in_at{0, 0u}, out_at{0, 0u};  // the next chunk to come, the next one to let go
+    double sums[3] = {0.0, 0.0, 0.0};
+    uint32_t live = 0;  // rows joined so far
+    auto let_go = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[out_at.slot]);
+      out_at.step();
+    };
+    auto vecs_of = [&](const Slice& s, int c) {
+      const int left = s.n - c * kChunkVecs;
+      return left < kChunkVecs ? left : kChunkVecs;
+    };
+    Token cur = load_token(a, first, rank == 0 && tid == 0);
+    bool ok = true;
+    while (cur.t < a.T) {
+      const Token next = load_token(a, cur.t + groups, rank == 0 && tid == 0);
+      const Slice sl = slice_of(cur.t);
+      // the entries outside whole vectors: threads 0-7 the head's, 8-15 the tail's, of rank 0
+      int edge = -1;
+      if (rank == 0 && tid < 16) {
+        if (tid < 8 && tid < sl.sh.head) edge = tid;
+        if (tid >= 8 && tid - 8 < sl.sh.tail) edge = static_cast<int>(a.V) - sl.sh.tail + (tid - 8);
+      }
+      float ez = 0.f;
+      RowGrad g{0.f, 0.f, 0.f, 0.f};
+      const bool counts = cur.w != 0.f;
+      const int again = !hold ? sl.chunks : sl.chunks > kRing ? sl.chunks - kRing : 0;
+      if (counts) {
+        RowSum s{-CUDART_INF_F, 0.f, 0.f};
+        TokenIn in{};
+        if (warp == 0) in = load_inputs<T>(a, cur);
+        if (edge >= 0) {
+          ez = to_f32<T>(row_of(cur.t)[edge]);
+          add_one(s, ez, scale);
+        }
+        for (int c = 0; c < sl.chunks; ++c) {
+          if (ok) ok = mbar_wait(&full[in_at.slot], in_at.round, abort_flag, a.status);
+          if (ok) sum_span<T, kThreads>(s, ring + in_at.slot * kChunkVecs, vecs_of(sl, c), tid, scale);
+          in_at.step();
+          if (c < again) let_go();
+        }
+        s = join_warp(s, scale);
+        const uint32_t half = live & 1u;
+        if (lane == 0) part[half][warp] = s;
+        named_bar_sync(kBarConsumers, kThreads);
+        if (warp == 0) {
+          s = lane < kWarps ? part[half][lane] : RowSum{-CUDART_INF_F, 0.f, 0.f};
+          s = join_warp(s, scale);
+          if (C > 1) {
+            // A peer one row ahead writes the other half of xchg, and none is two ahead.
+            if (lane < C) {
+              st_cluster_v4(mapa_shared(smem_u32(&xchg[half][rank]), lane), __float_as_uint(s.m),
+                            __float_as_uint(s.l), __float_as_uint(s.e), 0u);
+              arrive_cluster(&met[half], lane);
+            }
+            if (ok) ok = wait_cluster(&met[half], (live >> 1) & 1u, abort_flag, a.status);
+            const float4 x = lane < C ? xchg[half][lane] : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
+            s = join_warp(RowSum{x.x, x.y, x.z}, scale);
+          }
+          g = finish_token(a, cur, in, s, rank == 0 && lane == 0, sums);
+          if (lane == 0) row_grad = g;
+        }
+        ++live;
+      } else if (rank == 0 && tid == 0) {
+        if (a.logp != nullptr) a.logp[cur.t] = 0.f;
+        if (a.entropy != nullptr) a.entropy[cur.t] = 0.f;
+      }
+      if (hold) {
+        if (counts) {
+          named_bar_sync(kBarConsumers, kThreads);
+          g = row_grad;
+        }
+        const int start = sl.sh.head + v0 * E;
+        T* out = grad + cur.t * a.ld_grad + start;
+        if (counts) {
+          for (int i = again; i < sl.chunks + again; ++i) {
+            const int c = i < sl.chunks ? i : i - sl.chunks;
+            if (i >= sl.chunks) {
+              if (ok) ok = mbar_wait(&full[in_at.slot], in_at.round, abort_flag, a.status);
+              in_at.step();
+            }
+            const int e0 = c * kChunkVecs * E;
+            if (ok)
+              grad_span<T, kThreads>(ring + out_at.slot * kChunkVecs, out + e0, vecs_of(sl, c), tid, g, scale,
+                                     cur.target - start - e0);
+            let_go();
+          }
+        } else {
+          grad_span<T, kThreads>(nullptr, out, sl.n, tid, g, scale, -1);
+        }
+        if (edge >= 0)
+          grad[cur.t * a.ld_grad + edge] =
+              g.f != 0.f ? grad_one<T>(ez, g, scale, edge == cur.target) : from_f32<T>(0.f);
+      }
+      cur = next;
     }
-    __syncthreads();  // the slot, part and row_grad are free
-    if (kResident && tid == 0) issue(slots == 2 ? after : next, slot);
-    if (slots == 2) slot ^= 1;
-    cur = next;
-    next = after;
-  }
-  // a wait ran out: no copy may still be landing when the CTA leaves
-  if (kResident && tid == 0 && *abort_flag)
-    for (int s = 0; s < 2; ++s)
-      if (issued[s] > 0)
-        mbar_wait_slow(&full[s], (issued[s] - 1) & 1, nullptr, nullptr, kDrainLimitNs);
-  if (rank == 0 && tid == 0) {
-    if (groups == 1) {
-      write_loss(a, sums);
-    } else {
-      double* p = a.partial + first * 4;
+    if (rank == 0 && tid == 0) {
+      if (groups == 1) {
+        write_loss(a, sums);
+      } else {
+        double* p = a.partial + static_cast<int64_t>(first) * 4;
 #pragma unroll
-      for (int j = 0; j < 3; ++j) p[j] = sums[j];
+        for (int j = 0; j < 3; ++j) p[j] = sums[j];
+      }
     }
+  }
+  if (C > 1) {
+    __syncwarp();
+    cluster_sync();  // no peer writes here any more (every wait before is bounded)
   }
 }
 
@@ -511,15 +624,15 @@ __global__ void __launch_bounds__(kThreads) policy_warp_kernel(const PolicyArgs 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float scale = a.inv_temp * kLog2e;
   double sums[3] = {0.0, 0.0, 0.0};
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + warp; t < a.T;
-       t += static_cast<int64_t>(gridDim.x) * kWarps) {
+  for (int t = static_cast<int>(blockIdx.x) * kWarps + warp; t < a.T;
+       t += static_cast<int>(gridDim.x) * kWarps) {
     const Token k = load_token(a, t, lane == 0);
     const T* row = static_cast<const T*>(a.logits) + t * a.ld_logits;
-    const RowShape sh = row_shape(row, a.V);
+    const RowShape sh = row_shape(row, static_cast<int>(a.V));
     const uint4* src = reinterpret_cast<const uint4*>(row + sh.head);
-    int64_t edge = -1;
+    int edge = -1;
     if (lane < 8 && lane < sh.head) edge = lane;
-    if (lane >= 8 && lane - 8 < sh.tail) edge = a.V - sh.tail + (lane - 8);
+    if (lane >= 8 && lane - 8 < sh.tail) edge = static_cast<int>(a.V) - sh.tail + (lane - 8);
     float ez = 0.f;
     RowGrad g{0.f, 0.f, 0.f, 0.f};
     if (k.w != 0.f) {
@@ -583,22 +696,21 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(const PolicyArgs a, 
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-constexpr int64_t kSmemSm = 227 * 1024;  // shared memory of an SM that CTAs may take
-constexpr int64_t kSmemStatic = 2048;    // at most what a CTA takes beside its slots, with the reserve
+constexpr size_t kRingBytes = static_cast<size_t>(kRing) * kChunkBytes;
+constexpr int kCtasPerSm = 3;
+static_assert(kCtasPerSm * (kRingBytes + 2048) <= 227 * 1024, "three rings an SM");
 
 template <typename T>
 cudaError_t set_smem() {
-  // the kernel's limit, the same for every call
-  return cudaFuncSetAttribute(policy_cluster_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(kSmemSm - kSmemStatic));
+  return cudaFuncSetAttribute(policy_row_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(kRingBytes));
 }
 
-// Clusters of the resident kernel that run at once (0 on error), cached per device and launch shape.
+// Clusters of C CTAs of the row kernel that run at once (0 on error), cached per device and C.
 template <typename T>
-int active_clusters(int C, size_t smem) {
+int active_clusters(int C) {
   struct Entry {
     int dev, C, clusters;
-    size_t smem;
   };
   static std::mutex mu;
   static Entry cache[32];
@@ -607,11 +719,11 @@ int active_clusters(int C, size_t smem) {
   if (cudaGetDevice(&dev) != cudaSuccess) return 0;
   std::lock_guard<std::mutex> lock(mu);
   for (int i = 0; i < used; ++i)
-    if (cache[i].dev == dev && cache[i].C == C && cache[i].smem == smem) return cache[i].clusters;
+    if (cache[i].dev == dev && cache[i].C == C) return cache[i].clusters;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(C);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.blockDim = dim3(kRowThreads);
+  cfg.dynamicSmemBytes = kRingBytes;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C;
@@ -621,11 +733,11 @@ int active_clusters(int C, size_t smem) {
   cfg.numAttrs = 1;
   int n = 0;
   if (set_smem<T>() != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, policy_cluster_kernel<T, true>, &cfg) != cudaSuccess) {
+      cudaOccupancyMaxActiveClusters(&n, policy_row_kernel<T>, &cfg) != cudaSuccess) {
     (void)cudaGetLastError();
-    n = 0;
+    return 0;
   }
-  cache[used < 32 ? used++ : 31] = Entry{dev, C, n, smem};
+  if (used < 32) cache[used++] = Entry{dev, C, n};
   return n;
 }
 
@@ -642,24 +754,23 @@ cudaError_t launch(const PolicyArgs& a, int num_sms, cudaStream_t st) {
     parts = blocks;
     err = launch_pdl(policy_warp_kernel<T>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, 1, a);
   } else {
-    // Slices of which three CTAs an SM hold two each, in as narrow a cluster as gives them; a wider
-    // one while that puts idle SMs to work and leaves every thread a vector.
+    // A row that does not fit the rings is read again from L2: the rows in flight have to stay there
+    // (half of its 129 MB).  A wider cluster too while that puts idle CTAs to work and leaves every
+    // thread two vectors.
+    const int64_t resident = static_cast<int64_t>(num_sms) * kCtasPerSm;
     int C = 1;
-    while (C < kMaxCluster && (nvec + C - 1) / C * 16 * 6 > kSmemSm - 3 * kSmemStatic) C *= 2;
-    while (C < kMaxCluster && a.T * C * 2 <= num_sms && nvec >= C * 2 * kThreads) C *= 2;
-    const int64_t cap = (nvec + C - 1) / C;
-    const int64_t bytes = cap * 16;
-    const bool resident = bytes <= kSmemSm - kSmemStatic;
-    const int slots = 3 * (2 * bytes + kSmemStatic) <= kSmemSm ? 2 : 1;
-    const size_t smem = resident ? static_cast<size_t>(bytes * slots) : 0;
-    int64_t groups = resident ? active_clusters<T>(C, smem) : static_cast<int64_t>(num_sms) * 4 / C;
+    if (a.grad != nullptr)
+      while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * kRingBytes) &&
+             (a.T < resident / C ? a.T : resident / C) * nvec * 16 > (int64_t{64} << 20))
+        C *= 2;
+    while (C < kMaxCluster && a.T * C * 2 <= resident && nvec >= C * 4 * kThreads) C *= 2;
+    int64_t groups = active_clusters<T>(C);
     if (groups <= 0) return cudaErrorInvalidConfiguration;
     if (groups > a.T) groups = a.T;
     if (groups > kPolicyParts) groups = kPolicyParts;
     parts = groups;
-    const dim3 grid(static_cast<unsigned>(groups * C)), block(kThreads);
-    err = resident ? launch_pdl(policy_cluster_kernel<T, true>, grid, block, smem, st, C, a, C, cap, slots)
-                   : launch_pdl(policy_cluster_kernel<T, false>, grid, block, 0, st, C, a, C, cap, 1);
+    err = launch_pdl(policy_row_kernel<T>, dim3(static_cast<unsigned>(groups * C)), dim3(kRowThreads),
+                     kRingBytes, st, C, a, C, static_cast<int>((nvec + C - 1) / C));
   }
   if (err != cudaSuccess || parts == 1) return err;  // one cluster (block) writes the loss itself
   return launch_pdl(policy_finish_kernel, dim3(1), dim3(256), 0, st, 1, a, static_cast<int>(parts));
