@@ -8,9 +8,11 @@
 // depend on the target's log-probability alone, so a second pass over the row writes
 //   grad_v = f [v = a] - (f / l) exp(z_v - m),  f = grad_scale inv_temp c
 // (not exp(z - lse): where the row's values are large, lse = m + log l rounds to m).
-// Exponentials are powers of two of (logit - m) (inv_temp log2 e), m the largest logit: the
-// difference first, which is exact or nearly so and cannot overflow where a scaled logit could (a
-// row at the type's lowest value).
+// Exponentials are powers of two of logit scale - M, scale = inv_temp log2 e, one fused operation.  A
+// sum of positive terms is as exact relative to any M that neither overflows nor loses it, so M is 0
+// to begin with and is set to the entries' maximum (rounded: it shifts l and the target's term alike)
+// only where the sums over- or underrun it.  Where M itself would overflow (a row at the type's lowest
+// value) the difference logit - m is taken first.
 //
 // A row is read from HBM once.  A producer warp streams it, by bulk copies, through a ring of chunks
 // in shared memory, and the chunks that fit stay there between the passes.  Of a longer row the first
@@ -118,42 +120,83 @@ struct Vec<__nv_bfloat16> {
   }
 };
 
-// Running softmax sums over the logits above -inf: maximum m, and with y = (logit - m) scale
-// l = sum 2^y, e = sum 2^y y.  Nothing seen: m = -inf, l = 0.  A NaN or +inf makes l NaN.
+// Running softmax sums over the logits above -inf relative to the logit m: with y = logit scale - M(m),
+// l = sum 2^y, e = sum 2^y y.  Nothing seen: l = 0, and m means nothing.  A NaN or +inf makes l NaN.
 struct RowSum {
-  float m, l, e;
+  float m = 0.f, l = 0.f, e = 0.f;
 };
 
-// The sums relative to a larger maximum.
+// M(m) is m scale in 32 bits, unless that is too large to be subtracted safely: then NaN, and
+// y = (logit - m) scale.
+__device__ __forceinline__ float scaled_ref(float m, float scale) {
+  const float M = m * scale;
+  return fabsf(M) <= 1e37f ? M : __uint_as_float(0x7fc00000u);
+}
+__device__ __forceinline__ float power_of(float z, float m, float M, float scale) {
+  return M == M ? fmaf(z, scale, -M) : (z - m) * scale;
+}
+
+// The sums relative to another logit.
 __device__ __forceinline__ void raise(RowSum& s, float m, float scale) {
-  if (s.m == m) return;
-  const float gap = (s.m - m) * scale;
-  const float f = exp2_approx(gap);  // 0 from m = -inf
-  s.e = s.m == -CUDART_INF_F ? s.l * f : fmaf(gap, s.l, s.e) * f;
+  if (s.m == m || s.l == 0.f) {
+    s.m = m;
+    return;
+  }
+  const float from = scaled_ref(s.m, scale), to = scaled_ref(m, scale);
+  const float gap = from == from && to == to ? from - to : (s.m - m) * scale;
+  const float f = exp2_approx(gap);
+  s.e = f == 0.f ? s.l * f : fmaf(gap, s.l, s.e) * f;
   s.l *= f;
   s.m = m;
 }
 
 __device__ __forceinline__ void add_one(RowSum& s, float z, float scale) {
   if (z == -CUDART_INF_F) return;
-  if (z > s.m) raise(s, z, scale);
-  const float y = (z - s.m) * scale, p = exp2_approx(y);
+  if (z > s.m || s.l == 0.f) raise(s, z, scale);
+  const float y = power_of(z, s.m, scaled_ref(s.m, scale), scale), p = exp2_approx(y);
   s.l += p;
   s.e = fmaf(p, y, s.e);
 }
 
-// 16 entries: their maximum first, then powers relative to the running one.  Entries of -inf give
-// 0 inf in the second sum; it is taken again without them where it comes out NaN.
-template <typename T>
-__device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / Vec<T>::kElems],
-                                            float scale) {
-  constexpr int kVecs = 16 / Vec<T>::kElems, kPairs = Vec<T>::kElems / 2;
-  float top = Vec<T>::top(raw[0]);
+// Vectors src[v], src[v + stride], ... below n, kVecs of them at most, relative to their maximum or
+// s.m, whichever is larger (if s has sums); entries of -inf left out.
+template <typename T, int kVecs>
+__device__ __noinline__ RowSum add_careful(RowSum s, const uint4* src, int v, int stride, int n, float scale) {
+  constexpr int kPairs = Vec<T>::kElems / 2;
+  float top = -CUDART_INF_F;
 #pragma unroll
-  for (int j = 1; j < kVecs; ++j) top = fmaxf(top, Vec<T>::top(raw[j]));
-  if (top > s.m) raise(s, top, scale);
-  const float ref = s.m == -CUDART_INF_F ? 0.f : -s.m;
-  const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(ref, ref);
+  for (int j = 0; j < kVecs; ++j)
+    if (v + j * stride < n) top = fmaxf(top, Vec<T>::top(src[v + j * stride]));
+  if (top > s.m || s.l == 0.f) raise(s, top, scale);
+  const float M = scaled_ref(s.m, scale);
+#pragma unroll 1
+  for (int j = 0; j < kVecs; ++j) {
+    if (v + j * stride >= n) break;
+    uint64_t z[kPairs];
+    Vec<T>::pairs(src[v + j * stride], z);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      float x[2];
+      unpack2(z[i], x[0], x[1]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float y = power_of(x[h], s.m, M, scale), p = exp2_approx(y);
+        if (x[h] != -CUDART_INF_F) {
+          s.l += p;
+          s.e = p != 0.f ? fmaf(p, y, s.e) : s.e;
+        }
+      }
+    }
+  }
+  return s;
+}
+
+// The two sums over 16 entries relative to M, in the order of pairs.
+template <typename T>
+__device__ __forceinline__ void sum_16(const uint4 (&raw)[16 / Vec<T>::kElems], float M, float scale, float& l,
+                                       float& e) {
+  constexpr int kVecs = 16 / Vec<T>::kElems, kPairs = Vec<T>::kElems / 2;
+  const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-M, -M);
   uint64_t l2 = 0, e2 = 0;
 #pragma unroll
   for (int j = 0; j < kVecs; ++j) {
@@ -161,34 +204,38 @@ __device__ __forceinline__ void add_vectors(RowSum& s, const uint4 (&raw)[16 / V
     Vec<T>::pairs(raw[j], z);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-      const uint64_t x2 = mul2(add2(z[i], ref2), scale2);
+      const uint64_t y2 = fma2(z[i], scale2, ref2);
       float a, b;
-      unpack2(x2, a, b);
+      unpack2(y2, a, b);
       const uint64_t p2 = pack2(exp2_approx(a), exp2_approx(b));
       l2 = add2(l2, p2);
-      e2 = fma2(p2, x2, e2);
+      e2 = fma2(p2, y2, e2);
     }
   }
   float a, b;
   unpack2(l2, a, b);
-  s.l += a + b;
+  l = a + b;
   unpack2(e2, a, b);
-  float e = a + b;
-  if (e != e) {
-    e = 0.f;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      uint64_t z[kPairs];
-      Vec<T>::pairs(raw[j], z);
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        unpack2(mul2(add2(z[i], ref2), scale2), a, b);
-        if (a != -CUDART_INF_F) e = fmaf(exp2_approx(a), a, e);
-        if (b != -CUDART_INF_F) e = fmaf(exp2_approx(b), b, e);
-      }
-    }
+  e = a + b;
+}
+
+// 16 entries, the vectors src[v], src[v + stride], ... which are in raw.  They are summed relative to
+// s.m as it is; where that does not do (M is NaN, the sum is too large for it or so small that entries
+// that matter may have vanished, an entry of -inf made 0 inf of the second sum, an entry is NaN) they
+// go the careful way.  M: scaled_ref(s.m), kept by the caller.
+template <typename T>
+__device__ __forceinline__ void add_vectors(RowSum& s, float& M, const uint4 (&raw)[16 / Vec<T>::kElems],
+                                            const uint4* src, int v, int stride, int n, float scale) {
+  constexpr float kMost = 1.0995116e12f, kLeast = 8.6736174e-19f;  // 2^40, 2^-60
+  float l, e;
+  sum_16<T>(raw, M, scale, l, e);
+  if (l > kLeast && fmaf(e, 0.f, l) < kMost) {
+    s.l += l;
+    s.e += e;
+  } else {
+    s = add_careful<T, 16 / Vec<T>::kElems>(s, src, v, stride, n, scale);
+    M = scaled_ref(s.m, scale);
   }
-  s.e += e;
 }
 
 // Where a row lies: `head` entries before its first 16-byte boundary, nvec whole vectors, then
@@ -208,74 +255,106 @@ __device__ __forceinline__ RowShape row_shape(const T* row, int V) {
   return s;
 }
 
-// Sums over vectors src[0 .. n), thread `tid` of kStride taking each kStride-th.
-template <typename T, int kStride>
+template <typename T>
+__device__ __forceinline__ uint4 no_entries() {
+  return make_uint4(Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf);
+}
+
+// Sums over vectors src[0 .. n), thread `tid` of kStride taking each kStride-th.  kWhole vectors (a
+// multiple of 16 kStride entries) go without bounds.
+template <typename T, int kStride, int kWhole>
 __device__ __forceinline__ void sum_span(RowSum& s, const uint4* src, int n, int tid, float scale) {
   constexpr int kVecs = 16 / Vec<T>::kElems;
+  static_assert(kWhole % (kStride * kVecs) == 0, "whole steps");
+  float M = scaled_ref(s.m, scale);
+  if (n == kWhole) {
+#pragma unroll
+    for (int base = 0; base < kWhole; base += kStride * kVecs) {
+      uint4 raw[kVecs];
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) raw[j] = src[base + j * kStride + tid];
+      add_vectors<T>(s, M, raw, src, base + tid, kStride, n, scale);
+    }
+    return;
+  }
   for (int base = 0; base < n; base += kStride * kVecs) {
     uint4 raw[kVecs];
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
       const int v = base + j * kStride + tid;
-      raw[j] = v < n ? src[v]
-                     : make_uint4(Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf, Vec<T>::kNegInf);
+      raw[j] = v < n ? src[v] : no_entries<T>();
     }
-    add_vectors<T>(s, raw, scale);
+    add_vectors<T>(s, M, raw, src, base + tid, kStride, n, scale);
   }
 }
 
 // What the second pass needs of a row.
 struct RowGrad {
-  float f, fl, m, za;  // factor, factor / l, maximum, the target's logit
+  float f, fl, m, M, za;  // factor, factor / l, the sums' m and M(m), the target's logit
 };
 
 template <typename T>
 __device__ __forceinline__ T grad_one(float z, const RowGrad& g, float scale, bool target) {
-  return from_f32<T>(fmaf(-g.fl, exp2_approx((z - g.m) * scale), target ? g.f : 0.f));
+  return from_f32<T>(fmaf(-g.fl, exp2_approx(power_of(z, g.m, g.M, scale)), target ? g.f : 0.f));
 }
 
-// Gradient of vectors src[0 .. n) to out (entry `first` of the row on; 16-byte aligned or not).
-// f = 0 writes zeros and reads nothing.  `at`: the target's entry relative to src, or outside.
-template <typename T, int kStride>
-__device__ __forceinline__ void grad_span(const uint4* src, T* out, int n, int tid, const RowGrad& g,
-                                          float scale, int at) {
-  constexpr int E = Vec<T>::kElems, kPairs = E / 2;
-  if ((reinterpret_cast<uintptr_t>(out) & 15u) != 0) {  // rows of another alignment than the logits'
-    const T* one = reinterpret_cast<const T*>(src);
-    for (int i = tid; i < n * E; i += kStride)
-      out[i] = g.f != 0.f ? grad_one<T>(to_f32<T>(one[i]), g, scale, i == at) : from_f32<T>(0.f);
-    return;
-  }
-  uint4* dst = reinterpret_cast<uint4*>(out);
-  if (g.f == 0.f) {
-    for (int v = tid; v < n; v += kStride) __stcs(dst + v, make_uint4(0u, 0u, 0u, 0u));
-    return;
-  }
-  const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-g.m, -g.m), fl2 = pack2(-g.fl, -g.fl);
-#pragma unroll 2
-  for (int v = tid; v < n; v += kStride) {
-    uint64_t z[kPairs];
-    Vec<T>::pairs(src[v], z);
+// The gradient of one vector but for the target's f.
+template <typename T>
+__device__ __forceinline__ uint4 grad_vector(const uint4& v, const RowGrad& g, float scale) {
+  constexpr int kPairs = Vec<T>::kElems / 2;
+  const uint64_t scale2 = pack2(scale, scale), ref2 = pack2(-g.M, -g.M), fl2 = pack2(-g.fl, -g.fl);
+  uint64_t z[kPairs];
+  Vec<T>::pairs(v, z);
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      float a, b;
-      unpack2(mul2(add2(z[i], ref2), scale2), a, b);
-      z[i] = mul2(pack2(exp2_approx(a), exp2_approx(b)), fl2);
-    }
-    __stcs(dst + v, Vec<T>::from_pairs(z));
+  for (int i = 0; i < kPairs; ++i) {
+    float a, b;
+    unpack2(fma2(z[i], scale2, ref2), a, b);
+    z[i] = mul2(pack2(exp2_approx(a), exp2_approx(b)), fl2);
   }
-  if (at >= 0 && at < n * E && (at / E) % kStride == tid)  // by the thread that wrote its vector
+  return Vec<T>::from_pairs(z);
+}
+
+// Gradient of vectors 0 .. n - 1, which load(v) gives, to out (the entry of vector 0; 16-byte aligned
+// or not), thread `tid` of kStride taking each kStride-th.  f = 0 writes zeros and loads nothing.
+// `at`: the target's entry relative to out, or outside.
+template <typename T, int kStride, int kWhole, typename Load>
+__device__ __forceinline__ void grad_span(Load load, T* out, int n, int tid, const RowGrad& g, float scale,
+                                          int at) {
+  constexpr int E = Vec<T>::kElems;
+  if ((reinterpret_cast<uintptr_t>(out) & 15u) != 0 || (g.f != 0.f && g.M != g.M)) {
+    // rows of another alignment than the logits', rows whose M overflows
+    for (int v = tid; v < n; v += kStride) {
+      const uint4 w = g.f != 0.f ? load(v) : make_uint4(0u, 0u, 0u, 0u);
+      const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        out[v * E + i] = g.f != 0.f ? grad_one<T>(to_f32<T>(e[i]), g, scale, false) : from_f32<T>(0.f);
+    }
+  } else {
+    uint4* dst = reinterpret_cast<uint4*>(out);
+    if (g.f == 0.f) {
+      for (int v = tid; v < n; v += kStride) __stcs(dst + v, make_uint4(0u, 0u, 0u, 0u));
+    } else if (n == kWhole) {
+#pragma unroll
+      for (int v = 0; v < kWhole; v += kStride) __stcs(dst + v + tid, grad_vector<T>(load(v + tid), g, scale));
+    } else {
+      for (int v = tid; v < n; v += kStride) __stcs(dst + v, grad_vector<T>(load(v), g, scale));
+    }
+  }
+  if (g.f != 0.f && at >= 0 && at < n * E && (at / E) % kStride == tid)  // by the thread that wrote its vector
     out[at] = grad_one<T>(g.za, g, scale, true);
 }
 
 // ---- a warp's entries joined ------------------------------------------------------------------
-__device__ __forceinline__ RowSum join_warp(RowSum s, float scale) {
-  float m = s.m;
+// (of kLanes neighbouring lanes, in all of them)
+template <int kLanes>
+__device__ __forceinline__ RowSum join_lanes(RowSum s, float scale) {
+  float m = s.l == 0.f ? -CUDART_INF_F : s.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int o = kLanes / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   raise(s, m, scale);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = kLanes / 2; o > 0; o >>= 1) {
     s.l += __shfl_xor_sync(0xffffffffu, s.l, o);
     s.e += __shfl_xor_sync(0xffffffffu, s.e, o);
   }
@@ -288,40 +367,49 @@ struct Token {
   float w;  // 0: does not count (or beyond the batch)
   int target;
 };
-__device__ __forceinline__ Token load_token(const PolicyArgs& a, int t, bool flag) {
+__device__ __forceinline__ Token load_token(const PolicyArgs& a, int t) {
   Token k{t, 0.f, 0};
-  if (t >= a.T) return k;
-  k.w = a.weight != nullptr ? a.weight[t] : 1.f / static_cast<float>(a.T);
-  if (k.w == 0.f) return k;
-  k.target = a.target[t];
-  if (k.target < 0 || k.target >= a.V) {
+  if (t < a.T) {
+    k.w = a.weight != nullptr ? a.weight[t] : 1.f / static_cast<float>(a.T);
+    k.target = a.target[t];
+  }
+  return k;
+}
+// A target out of range counts as weight 0.  `flag`: this thread records it.
+__device__ __forceinline__ void check_token(const PolicyArgs& a, Token& k, bool flag) {
+  if (k.w != 0.f && (k.target < 0 || k.target >= a.V)) {
     k.w = 0.f;
     if (flag && a.status != nullptr) atomicOr(a.status, PR2_STATUS_BAD_INDEX);
   }
-  return k;
 }
 
 struct TokenIn {
   float A, old, ref, za;
 };
-template <typename T>
-__device__ __forceinline__ TokenIn load_inputs(const PolicyArgs& a, const Token& k) {
+// (all but za, which needs a checked token)
+__device__ __forceinline__ TokenIn load_inputs(const PolicyArgs& a, int t) {
   TokenIn in{0.f, 0.f, 0.f, 0.f};
-  if (k.w == 0.f) return in;
-  in.A = a.advantage[k.t];
-  if (a.logp_old != nullptr) in.old = a.logp_old[k.t];
-  if (a.logp_ref != nullptr) in.ref = a.logp_ref[k.t];
-  in.za = to_f32<T>(static_cast<const T*>(a.logits)[static_cast<int64_t>(k.t) * a.ld_logits + k.target]);
+  if (t < a.T) {
+    in.A = a.advantage[t];
+    if (a.logp_old != nullptr) in.old = a.logp_old[t];
+    if (a.logp_ref != nullptr) in.ref = a.logp_ref[t];
+  }
   return in;
+}
+template <typename T>
+__device__ __forceinline__ float load_target(const PolicyArgs& a, const Token& k) {
+  if (k.w == 0.f) return 0.f;
+  return to_f32<T>(static_cast<const T*>(a.logits)[static_cast<int64_t>(k.t) * a.ld_logits + k.target]);
 }
 
 // The token's terms from its row's sums: adds them to sums[] (policy part, KL part, clip flag, each
-// times the weight) and gives the row's gradient factors.  `write`: this thread stores logp, entropy.
+// times the weight) and gives the row's gradient factors.  `write`: this thread stores logp and
+// entropy and keeps the sums.
 __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token& k, const TokenIn& in,
-                                                const RowSum& s, bool write,
+                                                const RowSum& s, float scale, bool write,
                                                 double (&sums)[3]) {
-  RowGrad g{0.f, 0.f, 0.f, in.za};
-  if (s.m == -CUDART_INF_F && s.l == 0.f) {  // no entry above -inf
+  RowGrad g{0.f, 0.f, 0.f, 0.f, in.za};
+  if (s.l == 0.f) {  // no entry above -inf
     if (write) {
       if (a.logp != nullptr) a.logp[k.t] = -CUDART_INF_F;
       if (a.entropy != nullptr) a.entropy[k.t] = 0.f;
@@ -329,7 +417,8 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
     return g;
   }
   const float logl = logf(s.l);
-  const float logp = fmaf(in.za - s.m, a.inv_temp, -logl);
+  const float M = scaled_ref(s.m, scale);
+  const float logp = fmaf(power_of(in.za, s.m, M, scale), kLn2, -logl);
   if (write) {
     if (a.logp != nullptr) a.logp[k.t] = logp;
     if (a.entropy != nullptr) a.entropy[k.t] = fmaf(-kLn2, s.e / s.l, logl);
@@ -342,16 +431,21 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   const bool shut = A > 0.f ? r > hi : A < 0.f && r < lo;
   const float part = A == 0.f ? 0.f : (shut ? (A > 0.f ? hi : lo) : r) * A;
   float c = shut || A == 0.f ? 0.f : -r * A;
-  sums[0] -= k.w * part;
-  sums[2] += shut ? k.w : 0.f;
+  float kl = 0.f;
   if (a.logp_ref != nullptr) {
     const float gap = in.ref - logp, x = expm1f(gap);
-    sums[1] += k.w * (isinf(x) ? x : x - gap);
+    kl = isinf(x) ? x : x - gap;
     if (a.kl_coef > 0.f) c -= a.kl_coef * x;
+  }
+  if (write) {
+    sums[0] -= k.w * part;
+    sums[1] += k.w * kl;
+    sums[2] += shut ? k.w : 0.f;
   }
   g.f = k.w * c * a.inv_temp * a.grad_scale;
   g.fl = g.f / s.l;
   g.m = s.m;
+  g.M = M;
   return g;
 }
 
@@ -366,7 +460,14 @@ constexpr int kRing = 4;             // chunks of a CTA's ring
 constexpr int kChunkVecs = 1024;     // 16-byte vectors of a chunk
 constexpr int kChunkBytes = kChunkVecs * 16;
 constexpr int kRowThreads = kThreads + 32;  // eight consumer warps, one producer
-constexpr int kBarConsumers = 1;
+constexpr int kTokens = 2;  // token records ahead of the consumers
+
+// A row's token as the producer hands it to the consumers.
+struct TokenRecord {
+  float w;
+  int target;
+  TokenIn in;
+};
 
 // A place in the ring: slot and how often the ring went round (its parity).
 struct RingAt {
@@ -425,10 +526,12 @@ template <typename T>
 __global__ void __launch_bounds__(kRowThreads, 3)
     policy_row_kernel(const PolicyArgs a, int C, int cap) {
   extern __shared__ uint4 ring[];
-  __shared__ RowSum part[2][kWarps];
+  __shared__ float4 part[2][kWarps];
   __shared__ float4 xchg[2][kMaxCluster];
   __shared__ RowGrad row_grad;
-  __shared__ uint64_t full[kRing], empty[kRing], met[2];
+  __shared__ TokenRecord record[kTokens];
+  __shared__ uint64_t full[kRing], empty[kRing], met[2], told[kTokens], read[kTokens];
+  __shared__ uint64_t joined[2], graded;
   __shared__ int abort_flag_s;
   volatile int* abort_flag = &abort_flag_s;
   constexpr int E = Vec<T>::kElems;
@@ -440,8 +543,15 @@ __global__ void __launch_bounds__(kRowThreads, 3)
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], kWarps);
     }
-    mbar_init(&met[0], C);
-    mbar_init(&met[1], C);
+    for (int i = 0; i < kTokens; ++i) {
+      mbar_init(&told[i], 1);
+      mbar_init(&read[i], kWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&met[i], C);
+      mbar_init(&joined[i], kWarps);
+    }
+    mbar_init(&graded, 1);
     fence_mbar_init();
   }
   if (C > 1)
@@ -469,10 +579,23 @@ __global__ void __launch_bounds__(kRowThreads, 3)
     if (lane == 0) {
       RingAt at{0, 0u};
       uint32_t landing = 0, last_round = 0;  // slots with a copy issued, and its round
-      Token cur = load_token(a, first, false);
+      // a token's row number, weight and inputs are loaded two rows ahead, its target's logit one ahead
+      Token cur = load_token(a, first), next = load_token(a, first + groups);
+      TokenIn cur_in = load_inputs(a, first), next_in = load_inputs(a, first + groups);
+      check_token(a, cur, rank == 0);
+      cur_in.za = load_target<T>(a, cur);
+      uint32_t row = 0;
       bool ok = true;
       while (cur.t < a.T && ok) {
-        const Token next = load_token(a, cur.t + groups, false);
+        const Token after = load_token(a, next.t + groups);
+        const TokenIn after_in = load_inputs(a, next.t + groups);
+        check_token(a, next, rank == 0);
+        next_in.za = load_target<T>(a, next);
+        const int rec = row % kTokens;
+        ok = mbar_wait(&read[rec], ((row / kTokens) & 1u) ^ 1u, abort_flag, a.status);
+        if (!ok) break;
+        record[rec] = TokenRecord{cur.w, cur.target, cur_in};
+        mbar_arrive(&told[rec]);
         if (cur.w != 0.f) {
           const Slice s = slice_of(cur.t);
           const char* src = reinterpret_cast<const char*>(row_of(cur.t) + s.sh.head) + static_cast<int64_t>(v0) * 16;
@@ -491,6 +614,10 @@ __global__ void __launch_bounds__(kRowThreads, 3)
           }
         }
         cur = next;
+        cur_in = next_in;
+        next = after;
+        next_in = after_in;
+        ++row;
       }
       // no copy may still be landing when the CTA leaves (the consumers may have given up)
       for (int i = 0; i < kRing; ++i)
@@ -499,8 +626,12 @@ __global__ void __launch_bounds__(kRowThreads, 3)
     }
   } else {
     // ---------------- consumers ----------------
-    // (after a wait ran out, ok is false: the warp waits for no copy any more and skips the work, but
-    // goes the same way through the barriers that the others may be waiting at)
+    // Every wait is bounded and decided by the whole warp; a warp whose wait ran out leaves.  A warp is
+    // at most one row ahead of another (there are two token records), so two halves of part and
+    // joined are enough.
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.status)) != 0;
+    };
     const float scale = a.inv_temp * kLog2e;
     T* grad = static_cast<T*>(a.grad);
     RingAt in_at{0, 0u}, out_at{0, 0u};  // the next chunk to come, the next one to let go
@@ -515,10 +646,12 @@ __global__ void __launch_bounds__(kRowThreads, 3)
       const int left = s.n - c * kChunkVecs;
       return left < kChunkVecs ? left : kChunkVecs;
     };
-    Token cur = load_token(a, first, rank == 0 && tid == 0);
     bool ok = true;
-    while (cur.t < a.T) {
-      const Token next = load_token(a, cur.t + groups, rank == 0 && tid == 0);
+    uint32_t turn = 0;
+    for (int t = first; t < a.T; t += groups, ++turn) {
+      const int rec = turn % kTokens;
+      if (!wait(&told[rec], (turn / kTokens) & 1u)) break;
+      const Token cur{t, record[rec].w, record[rec].target};
       const Slice sl = slice_of(cur.t);
       // the entries outside whole vectors: threads 0-7 the head's, 8-15 the tail's, of rank 0
       int edge = -1;
@@ -527,30 +660,30 @@ __global__ void __launch_bounds__(kRowThreads, 3)
         if (tid >= 8 && tid - 8 < sl.sh.tail) edge = static_cast<int>(a.V) - sl.sh.tail + (tid - 8);
       }
       float ez = 0.f;
-      RowGrad g{0.f, 0.f, 0.f, 0.f};
+      RowGrad g{0.f, 0.f, 0.f, 0.f, 0.f};
       const bool counts = cur.w != 0.f;
       const int again = !hold ? sl.chunks : sl.chunks > kRing ? sl.chunks - kRing : 0;
       if (counts) {
-        RowSum s{-CUDART_INF_F, 0.f, 0.f};
-        TokenIn in{};
-        if (warp == 0) in = load_inputs<T>(a, cur);
-        if (edge >= 0) {
-          ez = to_f32<T>(row_of(cur.t)[edge]);
-          add_one(s, ez, scale);
-        }
+        RowSum s;
+        if (edge >= 0) ez = to_f32<T>(row_of(cur.t)[edge]);
         for (int c = 0; c < sl.chunks; ++c) {
-          if (ok) ok = mbar_wait(&full[in_at.slot], in_at.round, abort_flag, a.status);
-          if (ok) sum_span<T, kThreads>(s, ring + in_at.slot * kChunkVecs, vecs_of(sl, c), tid, scale);
+          if (!(ok = wait(&full[in_at.slot], in_at.round))) break;
+          sum_span<T, kThreads, kChunkVecs>(s, ring + in_at.slot * kChunkVecs, vecs_of(sl, c), tid, scale);
           in_at.step();
           if (c < again) let_go();
         }
-        s = join_warp(s, scale);
+        if (!ok) break;
+        if (edge >= 0) add_one(s, ez, scale);
+        s = join_lanes<32>(s, scale);
         const uint32_t half = live & 1u;
-        if (lane == 0) part[half][warp] = s;
-        named_bar_sync(kBarConsumers, kThreads);
+        if (lane == 0) {
+          part[half][warp] = make_float4(s.m, s.l, s.e, 0.f);
+          mbar_arrive(&joined[half]);
+        }
         if (warp == 0) {
-          s = lane < kWarps ? part[half][lane] : RowSum{-CUDART_INF_F, 0.f, 0.f};
-          s = join_warp(s, scale);
+          if (!wait(&joined[half], (live >> 1) & 1u)) break;
+          const float4 own = part[half][lane % kWarps];
+          s = join_lanes<kWarps>(RowSum{own.x, own.y, own.z}, scale);
           if (C > 1) {
             // A peer one row ahead writes the other half of xchg, and none is two ahead.
             if (lane < C) {
@@ -558,12 +691,20 @@ __global__ void __launch_bounds__(kRowThreads, 3)
                             __float_as_uint(s.l), __float_as_uint(s.e), 0u);
               arrive_cluster(&met[half], lane);
             }
-            if (ok) ok = wait_cluster(&met[half], (live >> 1) & 1u, abort_flag, a.status);
-            const float4 x = lane < C ? xchg[half][lane] : make_float4(-CUDART_INF_F, 0.f, 0.f, 0.f);
-            s = join_warp(RowSum{x.x, x.y, x.z}, scale);
+            if (!__all_sync(0xffffffffu, wait_cluster(&met[half], (live >> 1) & 1u, abort_flag, a.status))) break;
+            const int r = lane % kMaxCluster;
+            const float4 x = r < C ? xchg[half][r] : make_float4(0.f, 0.f, 0.f, 0.f);
+            s = join_lanes<kMaxCluster>(RowSum{x.x, x.y, x.z}, scale);
           }
-          g = finish_token(a, cur, in, s, rank == 0 && lane == 0, sums);
-          if (lane == 0) row_grad = g;
+          g = finish_token(a, cur, record[rec].in, s, scale, rank == 0 && lane == 0, sums);
+          if (hold && lane == 0) {
+            row_grad = g;
+            mbar_arrive(&graded);
+          }
+        }
+        if (hold) {
+          if (!wait(&graded, live & 1u)) break;
+          g = row_grad;
         }
         ++live;
       } else if (rank == 0 && tid == 0) {
@@ -571,33 +712,30 @@ __global__ void __launch_bounds__(kRowThreads, 3)
         if (a.entropy != nullptr) a.entropy[cur.t] = 0.f;
       }
       if (hold) {
-        if (counts) {
-          named_bar_sync(kBarConsumers, kThreads);
-          g = row_grad;
-        }
         const int start = sl.sh.head + v0 * E;
         T* out = grad + cur.t * a.ld_grad + start;
         if (counts) {
           for (int i = again; i < sl.chunks + again; ++i) {
             const int c = i < sl.chunks ? i : i - sl.chunks;
             if (i >= sl.chunks) {
-              if (ok) ok = mbar_wait(&full[in_at.slot], in_at.round, abort_flag, a.status);
+              if (!(ok = wait(&full[in_at.slot], in_at.round))) break;
               in_at.step();
             }
             const int e0 = c * kChunkVecs * E;
-            if (ok)
-              grad_span<T, kThreads>(ring + out_at.slot * kChunkVecs, out + e0, vecs_of(sl, c), tid, g, scale,
-                                     cur.target - start - e0);
+            grad_span<T, kThreads, kChunkVecs>([&](int v) { return ring[out_at.slot * kChunkVecs + v]; }, out + e0,
+                                   vecs_of(sl, c), tid, g, scale, cur.target - start - e0);
             let_go();
           }
+          if (!ok) break;
         } else {
-          grad_span<T, kThreads>(nullptr, out, sl.n, tid, g, scale, -1);
+          grad_span<T, kThreads, kChunkVecs>([](int) { return make_uint4(0u, 0u, 0u, 0u); }, out, sl.n, tid, g, scale, -1);
         }
         if (edge >= 0)
           grad[cur.t * a.ld_grad + edge] =
               g.f != 0.f ? grad_one<T>(ez, g, scale, edge == cur.target) : from_f32<T>(0.f);
       }
-      cur = next;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&read[rec]);
     }
     if (rank == 0 && tid == 0) {
       if (groups == 1) {
@@ -615,44 +753,61 @@ __global__ void __launch_bounds__(kRowThreads, 3)
   }
 }
 
-// ---- a warp per row ------------------------------------------------------------------------------
-template <typename T>
-__global__ void __launch_bounds__(kThreads) policy_warp_kernel(const PolicyArgs a) {
+// ---- a warp per row --------------------------------------------------------------------------------
+// A lane holds up to kHeld vectors of the row between the passes.
+template <typename T, int kHeld>
+__global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kernel(const PolicyArgs a) {
+  constexpr int kVecs = 16 / Vec<T>::kElems;
   __shared__ double part[kWarps][3];
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float scale = a.inv_temp * kLog2e;
   double sums[3] = {0.0, 0.0, 0.0};
-  for (int t = static_cast<int>(blockIdx.x) * kWarps + warp; t < a.T;
-       t += static_cast<int>(gridDim.x) * kWarps) {
-    const Token k = load_token(a, t, lane == 0);
+  const int rows = static_cast<int>(gridDim.x) * kWarps;
+  for (int t = static_cast<int>(blockIdx.x) * kWarps + warp; t < a.T; t += rows) {
+    Token k = load_token(a, t);
     const T* row = static_cast<const T*>(a.logits) + t * a.ld_logits;
     const RowShape sh = row_shape(row, static_cast<int>(a.V));
     const uint4* src = reinterpret_cast<const uint4*>(row + sh.head);
+    check_token(a, k, lane == 0);
     int edge = -1;
     if (lane < 8 && lane < sh.head) edge = lane;
     if (lane >= 8 && lane - 8 < sh.tail) edge = static_cast<int>(a.V) - sh.tail + (lane - 8);
     float ez = 0.f;
-    RowGrad g{0.f, 0.f, 0.f, 0.f};
+    RowGrad g{0.f, 0.f, 0.f, 0.f, 0.f};
+    uint4 raw[kHeld];
     if (k.w != 0.f) {
-      RowSum s{-CUDART_INF_F, 0.f, 0.f};
-      const TokenIn in = load_inputs<T>(a, k);
-      if (edge >= 0) {
-        ez = to_f32<T>(row[edge]);
-        add_one(s, ez, scale);
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int v = j * 32 + lane;
+        raw[j] = v < sh.nvec ? src[v] : no_entries<T>();
       }
-      sum_span<T, 32>(s, src, sh.nvec, lane, scale);
-      s = join_warp(s, scale);
-      g = finish_token(a, k, in, s, lane == 0, sums);
+      RowSum s;
+      float M = scaled_ref(s.m, scale);
+      TokenIn in = load_inputs(a, t);
+      in.za = load_target<T>(a, k);
+      if (edge >= 0) ez = to_f32<T>(row[edge]);
+#pragma unroll
+      for (int j = 0; j < kHeld; j += kVecs)
+        if (j * 32 < sh.nvec) 
+          add_vectors<T>(s, M, reinterpret_cast<const uint4(&)[kVecs]>(raw[j]), src, j * 32 + lane, 32, sh.nvec, scale);
+      if (edge >= 0) add_one(s, ez, scale);
+      s = join_lanes<32>(s, scale);
+      g = finish_token(a, k, in, s, scale, lane == 0, sums);
     } else if (lane == 0) {
       if (a.logp != nullptr) a.logp[t] = 0.f;
       if (a.entropy != nullptr) a.entropy[t] = 0.f;
     }
     if (a.grad != nullptr) {
-      __syncwarp();  // (in place: the target's logit has been read)
+      __syncwarp();  // (in place: every lane has read the target's logit)
       T* out = static_cast<T*>(a.grad) + t * a.ld_grad;
-      grad_span<T, 32>(src, out + sh.head, sh.nvec, lane, g, scale, k.target - sh.head);
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int left = sh.nvec - j * 32, e0 = sh.head + j * 32 * Vec<T>::kElems;
+        if (left > 0)
+          grad_span<T, 32, 32>([&](int) { return raw[j]; }, out + e0, left < 32 ? left : 32, lane, g, scale, k.target - e0);
+      }
       if (edge >= 0)
         out[edge] = g.f != 0.f ? grad_one<T>(ez, g, scale, edge == k.target) : from_f32<T>(0.f);
     }
@@ -745,23 +900,28 @@ template <typename T>
 cudaError_t launch(const PolicyArgs& a, int num_sms, cudaStream_t st) {
   constexpr int E = Vec<T>::kElems;
   const int64_t nvec = a.V / E;  // most whole vectors of a row
+  const int64_t resident = static_cast<int64_t>(num_sms) * kCtasPerSm;
   int64_t parts;
   cudaError_t err;
-  if (nvec <= 256) {  // at most 8 vectors a lane
+  // A warp a row up to 4 KB, and up to 8 KB where the rows outnumber the CTAs that the row kernel keeps
+  // resident (bf16 rows of 4096, us: 256 rows 11.3 by warps, 8.8 by rows; 2432 rows 13.3 / 24.6; rows
+  // of 8192, 2432 of them 31 / 25).
+  if (nvec <= 256 || (nvec <= 512 && a.T > resident)) {
     int64_t blocks = (a.T + kWarps - 1) / kWarps;
-    const int64_t cap = static_cast<int64_t>(num_sms) * 8;
-    if (blocks > cap) blocks = cap;
+    if (blocks > kPolicyParts) blocks = kPolicyParts;
     parts = blocks;
-    err = launch_pdl(policy_warp_kernel<T>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, 1, a);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    err = nvec <= 128 ? launch_pdl(policy_warp_kernel<T, 4>, grid, dim3(kThreads), 0, st, 1, a)
+          : nvec <= 256 ? launch_pdl(policy_warp_kernel<T, 8>, grid, dim3(kThreads), 0, st, 1, a)
+                      : launch_pdl(policy_warp_kernel<T, 16>, grid, dim3(kThreads), 0, st, 1, a);
   } else {
     // A row that does not fit the rings is read again from L2: the rows in flight have to stay there
-    // (half of its 129 MB).  A wider cluster too while that puts idle CTAs to work and leaves every
+    // (with the gradients on their way, 48 of its 129 MB).  A wider cluster too while that puts idle CTAs to work and leaves every
     // thread two vectors.
-    const int64_t resident = static_cast<int64_t>(num_sms) * kCtasPerSm;
     int C = 1;
     if (a.grad != nullptr)
       while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * kRingBytes) &&
-             (a.T < resident / C ? a.T : resident / C) * nvec * 16 > (int64_t{64} << 20))
+             (a.T < resident / C ? a.T : resident / C) * nvec * 16 > (int64_t{48} << 20))
         C *= 2;
     while (C < kMaxCluster && a.T * C * 2 <= resident && nvec >= C * 4 * kThreads) C *= 2;
     int64_t groups = active_clusters<T>(C);
