@@ -493,6 +493,27 @@ __device__ __forceinline__ uint32_t lanemask_lt() {
   return m;
 }
 
+// Items i, i + step, i + 2 step, ... of rows of `n` items each, as (row, column): one division at the
+// start instead of one an item.
+struct RowWalk {
+  int64_t row, row_step;
+  int col, col_step, n;
+  __device__ __forceinline__ RowWalk(int64_t i, int64_t step, int n_) : n(n_) {
+    row = i / n;
+    col = static_cast<int>(i - row * n);
+    row_step = step / n;
+    col_step = static_cast<int>(step - row_step * n);
+  }
+  __device__ __forceinline__ void next() {
+    row += row_step;
+    col += col_step;
+    if (col >= n) {
+      col -= n;
+      ++row;
+    }
+  }
+};
+
 // Sum of each v[j] (j < 8) over the warp: returned in the lanes whose bits 4, 3, 2 are j.
 __device__ __forceinline__ float warp_sum8(const float (&v)[8]) {
   const int lane = threadIdx.x & 31;

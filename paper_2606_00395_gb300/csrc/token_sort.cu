@@ -108,11 +108,11 @@ __global__ void __launch_bounds__(kThreads)
       perm[r] = -1;
   if (x == nullptr) return;
   const int pieces = (n + 32 * U - 1) / (32 * U);
-  const int64_t items = static_cast<int64_t>(Tn) * pieces;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); i < items;
-       i += static_cast<int64_t>(gridDim.x) * kWarps) {
-    const int64_t t = i / pieces;
-    const int c0 = static_cast<int>(i - t * pieces) * 32 * U + lane;
+  RowWalk at(static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x) * kWarps,
+             pieces);
+  for (; at.row < Tn; at.next()) {
+    const int64_t t = at.row;
+    const int c0 = at.col * 32 * U + lane;
     typename L::Raw v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -143,6 +143,8 @@ __global__ void __launch_bounds__(kThreads)
   pdl_trigger();
   const int F = Tn * k, lane = threadIdx.x & 31, n = d / V;
   const int pieces = (n + 32 * U - 1) / (32 * U);
+  // (a division an item: its operands take fewer registers than a running row and column, and the loads
+  // in flight need them)
   const int64_t items = static_cast<int64_t>(Tn) * pieces;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); i < items;
        i += static_cast<int64_t>(gridDim.x) * kWarps) {

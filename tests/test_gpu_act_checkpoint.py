@@ -66,7 +66,8 @@ def check_backward(got, q, scale, dact, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("Rn,m,extra,shift", [
     (1, 1, 0, 0), (1, 127, 0, 0), (3, 128, 0, 0), (5, 129, 1, 1), (2, 768, 768, 0), (700, 768, 0, 0), (33, 1000, 0, 0),
-    (33, 1000, 1000, 4), (9, 1001, 0, 0), (4, 4096, 8, 8), (3000, 72, 0, 0), (257, 16, 16, 0), (2, 20000, 0, 0)])
+    (33, 1000, 1000, 4), (9, 1001, 0, 0), (4, 4096, 8, 8), (3000, 72, 0, 0), (257, 16, 16, 0), (2, 20000, 0, 0),
+    (7, 136, 0, 0), (31, 8, 0, 0), (400, 264, 8, 0)])
 def test_checkpoint_and_backward(Rn, m, extra, shift, dtype):
     gate, up, dact = inputs(Rn, m, dtype, Rn + m)
     ld = m + extra
