@@ -7,10 +7,13 @@
 // order are found through inv, so nothing is written twice and the sums do not depend on the launch
 // but for the split of a row over warps.  Rows past offsets[N], which no slot names, are zeroed.
 // A row number outside [0, T k) is taken as an invalid slot.
+// The plan of up to 8192 slots is made by one cluster (plan_kernel), of more by the layer forward's
+// dispatch.
 //
 // All of it is bound by HBM: the k expert rows, read or written once.  A warp takes a piece of a
 // token's row, a lane V neighbouring columns: 16 bytes where d and the pointers allow it, else one
-// element (a row of odd width starts at any element).
+// fp32 element or a pair of bf16 ones (a row of odd width starts at any element, so a row's pairs
+// start at its first column or at its second, whichever lies on 4 bytes).
 #include "pr2_device.cuh"
 #include "pr2_internal.h"
 
@@ -23,16 +26,22 @@ constexpr int kSlots = 8;  // slots handled at once; more go in further rounds
 
 template <typename T, int V>
 struct Lane;  // V elements: 16 bytes, or one
-template <typename T>
-struct Lane<T, 1> {
-  using Raw = T;
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[1]) { f[0] = to_f32<T>(r); }
-  static __device__ __forceinline__ Raw pack(const float (&f)[1]) { return from_f32<T>(f[0]); }
-  static __device__ __forceinline__ Raw zero() { return from_f32<T>(0.f); }
+template <>
+struct Lane<float, 1> {
+  using Raw = float;
+  using Held = float;  // a Raw on its way (in a register of its own)
+  static __device__ __forceinline__ void unpack(Held r, float (&f)[1]) { f[0] = r; }
+  static __device__ __forceinline__ Raw pack(const float (&f)[1]) { return f[0]; }
+  static __device__ __forceinline__ Held load(const Raw* p) { return __ldg(p); }
+  static __device__ __forceinline__ Raw raw(Held r) { return r; }
+  static __device__ __forceinline__ Raw zero() { return 0.f; }
 };
 template <>
 struct Lane<float, 4> {
   using Raw = uint4;
+  using Held = uint4;
+  static __device__ __forceinline__ Held load(const Raw* p) { return __ldcs(p); }
+  static __device__ __forceinline__ Raw raw(const Held& r) { return r; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[4]) {
     f[0] = __uint_as_float(r.x);
     f[1] = __uint_as_float(r.y);
@@ -47,6 +56,9 @@ struct Lane<float, 4> {
 template <>
 struct Lane<__nv_bfloat16, 8> {
   using Raw = uint4;
+  using Held = uint4;
+  static __device__ __forceinline__ Held load(const Raw* p) { return __ldcs(p); }
+  static __device__ __forceinline__ Raw raw(const Held& r) { return r; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&f)[8]) {
     const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -83,11 +95,107 @@ __device__ __forceinline__ int rows_used(const int32_t* __restrict__ offsets, in
   return n < 0 ? 0 : n < F ? n : F;
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void zero_rows(T* x, int from, int F, int d) {
-  const int n = d / V;
+// Rows from .. F - 1 of n Raws each.
+template <typename Raw>
+__device__ __forceinline__ void zero_rows(Raw* x, int from, int F, int n) {
   for (int r = from + blockIdx.x; r < F; r += gridDim.x)
-    for (int c = threadIdx.x; c < n; c += kThreads) lanes_of<T, V>(x + static_cast<int64_t>(r) * d)[c] = Lane<T, V>::zero();
+    for (int c = threadIdx.x; c < n; c += kThreads) x[static_cast<int64_t>(r) * n + c] = Raw{};
+}
+__device__ __forceinline__ void fill_perm(int32_t* __restrict__ perm, int from, int F) {
+  if (perm == nullptr) return;
+  for (int64_t r = from + static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; r < F;
+       r += static_cast<int64_t>(gridDim.x) * kThreads)
+    perm[r] = -1;
+}
+
+// ---- the plan of a batch of up to kPlanSlots slots -----------------------------------------------------
+// One cluster, a slot per thread: counts per warp and expert by __match_any_sync, summed per block, the
+// blocks' counts exchanged through distributed shared memory; then every block scans the experts'
+// totals and places its slots in order.  No memory outside the cluster is waited for, so it is an
+// ordinary launch.  Latency-bound: 2048 slots of 128 experts take about 4 us where the dispatch's
+// cooperative launch and the clearing of its counters take 9.
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanBlocks = 8;
+static_assert(kPlanThreads * kPlanBlocks == kPlanSlots, "a slot per thread");
+
+__global__ void __launch_bounds__(kPlanThreads)
+    plan_kernel(const int32_t* __restrict__ idx, int F, int k, int N, int blocks, int32_t* __restrict__ offsets,
+                int32_t* __restrict__ perm, int32_t* __restrict__ inv, int32_t* __restrict__ status) {
+  extern __shared__ int plan_smem[];
+  int* before = plan_smem;                        // [32][N] slots of the expert in earlier warps
+  int* counts = before + 32 * N;                  // [kPlanBlocks][N]
+  int* first = counts + kPlanBlocks * N;          // [N] row of the block's first slot of the expert
+  __shared__ int warp_sum[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = blocks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  for (int i = tid; i < 32 * N; i += kPlanThreads) before[i] = 0;
+  if (blocks > 1) cluster_sync();  // peers write to counts
+  pdl_wait();
+  pdl_trigger();
+  const int f = rank * kPlanThreads + tid;
+  int e = f < F ? idx[f] : -1;
+  if (e < 0 || e >= N) e = -1;
+  for (int g = f - f % k; g < f && e >= 0; ++g)
+    if (idx[g] == e) e = -1;  // repeated within its token
+  if (f < F && e < 0 && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
+  __syncthreads();
+  const unsigned same = __match_any_sync(0xffffffffu, e);
+  if (e >= 0 && lane == __ffs(same) - 1) before[warp * N + e] = __popc(same);
+  __syncthreads();
+  if (tid < N) {
+    int sum = 0;
+    for (int w = 0; w < 32; ++w) {
+      const int c = before[w * N + tid];
+      before[w * N + tid] = sum;
+      sum += c;
+    }
+    for (int b = 0; b < blocks; ++b) {
+      const uint32_t at = smem_u32(&counts[rank * N + tid]);
+      if (blocks > 1)
+        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(mapa_shared(at, b)), "r"(sum) : "memory");
+      else
+        counts[tid] = sum;
+    }
+  }
+  if (blocks > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  int all = 0, mine = 0;
+  if (tid < N)
+    for (int b = 0; b < blocks; ++b) {
+      const int c = counts[b * N + tid];
+      mine += b < rank ? c : 0;
+      all += c;
+    }
+  int scan = all;  // inclusive over the experts
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_sum[warp] = scan;
+  __syncthreads();
+  int earlier = 0, used = 0;
+  for (int w = 0; w < kMaxExperts / 32; ++w) {
+    earlier += w < warp ? warp_sum[w] : 0;
+    used += warp_sum[w];
+  }
+  if (tid < N) {
+    const int off = earlier + scan - all;
+    first[tid] = off + mine;
+    if (rank == 0) offsets[tid] = off;
+  }
+  if (rank == 0 && tid == 0) offsets[N] = used;
+  __syncthreads();
+  if (f >= F) return;
+  int row = -1;
+  if (e >= 0) {
+    row = first[e] + before[warp * N + e] + __popc(same & lanemask_lt());
+    perm[row] = f;
+  }
+  inv[f] = row;
+  if (f >= used) perm[f] = -1;
 }
 
 // ---- sort: a warp per (token, U lanes' worth of its columns) ---------------------------------------
@@ -102,21 +210,18 @@ __global__ void __launch_bounds__(kThreads)
   if (status_timed_out(status)) return;  // dispatch gave up: its tables may be unwritten
   const int F = Tn * k, lane = threadIdx.x & 31, n = d / V;
   const int used = rows_used(offsets, N, F);
-  if (perm != nullptr)
-    for (int64_t r = used + static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; r < F;
-         r += static_cast<int64_t>(gridDim.x) * kThreads)
-      perm[r] = -1;
-  if (x == nullptr) return;
+  fill_perm(perm, used, F);
+  if (x == nullptr) return;  // the plan alone
   const int pieces = (n + 32 * U - 1) / (32 * U);
   RowWalk at(static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x) * kWarps,
              pieces);
   for (; at.row < Tn; at.next()) {
     const int64_t t = at.row;
     const int c0 = at.col * 32 * U + lane;
-    typename L::Raw v[U];
+    typename L::Held v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (c0 + u * 32 < n) v[u] = __ldg(lanes_of<T, V>(h + t * d) + c0 + u * 32);
+      if (c0 + u * 32 < n) v[u] = L::load(lanes_of<T, V>(h + t * d) + c0 + u * 32);
     for (int s0 = 0; s0 < k; s0 += kSlots) {
       const int mine = lane < kSlots ? my_row(inv, t, k, s0 + lane, F) : -1;
 #pragma unroll
@@ -126,11 +231,11 @@ __global__ void __launch_bounds__(kThreads)
         auto* dst = lanes_of<T, V>(x + static_cast<int64_t>(r) * d);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (c0 + u * 32 < n) __stcs(dst + c0 + u * 32, v[u]);
+          if (c0 + u * 32 < n) __stcs(dst + c0 + u * 32, L::raw(v[u]));
       }
     }
   }
-  zero_rows<T, V>(x, used, F, d);
+  zero_rows(lanes_of<T, V>(x), used, F, n);
 }
 
 // ---- sums of a token's rows (unsort; sort_backward: gates NULL, all 1) ------------------------------
@@ -158,13 +263,13 @@ __global__ void __launch_bounds__(kThreads)
     for (int s0 = 0; s0 < k; s0 += kSlots) {
       const int mine = lane < kSlots ? my_row(inv, t, k, s0 + lane, F) : -1;
       const float my_g = lane < kSlots && s0 + lane < k && gates != nullptr ? gates[t * k + s0 + lane] : 1.f;
-      typename L::Raw raw[kSlots][U];
+      typename L::Held raw[kSlots][U];
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) {
         const int r = __shfl_sync(0xffffffffu, mine, s);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          raw[s][u] = r >= 0 && c0 + u * 32 < n ? __ldcs(lanes_of<T, V>(y + static_cast<int64_t>(r) * d) + c0 + u * 32)
+          raw[s][u] = r >= 0 && c0 + u * 32 < n ? L::load(lanes_of<T, V>(y + static_cast<int64_t>(r) * d) + c0 + u * 32)
                                                 : L::zero();
       }
 #pragma unroll
@@ -185,6 +290,29 @@ __global__ void __launch_bounds__(kThreads)
     for (int u = 0; u < U; ++u)
       if (c0 + u * 32 < n) lanes_of<T, V>(out + t * d)[c0 + u * 32] = L::pack(acc[u]);
   }
+}
+
+// Gates' gradients of a token's slots s0 .. s0 + 7 from its G warps' partial sums (every thread of the
+// block calls this if G > 1).
+template <int G>
+__device__ __forceinline__ void write_gate_grads(const float (&acc)[kSlots], int64_t t, bool valid, int s0, int k,
+                                                 float (*part)[kSlots], float* __restrict__ dgates) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float sum = warp_sum8(acc);  // of slot s in the lanes whose bits 4, 3, 2 are s
+  const int s = lane >> 2;
+  if (G == 1) {
+    if ((lane & 3) == 0 && s0 + s < k) dgates[t * k + s0 + s] = sum;
+    return;
+  }
+  if ((lane & 3) == 0) part[warp][s] = sum;
+  __syncthreads();
+  if (warp % G == 0 && lane < kSlots && valid && s0 + lane < k) {
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < G; ++w) all += part[warp + w][lane];
+    dgates[t * k + s0 + lane] = all;
+  }
+  __syncthreads();
 }
 
 // ---- unsort_backward: G warps a token -----------------------------------------------------------------
@@ -214,17 +342,17 @@ __global__ void __launch_bounds__(kThreads)
       for (int s = 0; s < kSlots; ++s) acc[s] = 0.f;
       if (t < Tn)
         for (int c0 = g_warp * 32 * U + lane; c0 - lane < n; c0 += G * 32 * U) {
-          typename L::Raw raw[kSlots][U], own_raw[U];
+          typename L::Held raw[kSlots][U], own_raw[U];
 #pragma unroll
           for (int u = 0; u < U; ++u)
-            own_raw[u] = c0 + u * 32 < n ? __ldg(lanes_of<T, V>(dout + t * d) + c0 + u * 32) : L::zero();
+            own_raw[u] = c0 + u * 32 < n ? L::load(lanes_of<T, V>(dout + t * d) + c0 + u * 32) : L::zero();
 #pragma unroll
           for (int s = 0; s < kSlots; ++s) {
             const int r = __shfl_sync(0xffffffffu, mine, s);
 #pragma unroll
             for (int u = 0; u < U; ++u)
               raw[s][u] = r >= 0 && c0 + u * 32 < n
-                              ? __ldcs(lanes_of<T, V>(y + static_cast<int64_t>(r) * d) + c0 + u * 32)
+                              ? L::load(lanes_of<T, V>(y + static_cast<int64_t>(r) * d) + c0 + u * 32)
                               : L::zero();
           }
 #pragma unroll
@@ -247,26 +375,197 @@ __global__ void __launch_bounds__(kThreads)
             }
           }
         }
-      // sum of slot s in the lanes whose bits 4, 3, 2 are s
-      const float sum = warp_sum8(acc);
-      const int s = (lane >> 2) & 7;
-      const bool writes = (lane & 3) == 0;
-      if (G == 1) {
-        if (writes && s0 + s < k) dgates[t * k + s0 + s] = sum;
-      } else {
-        if (writes) part[warp][s] = sum;
-        __syncthreads();
-        if (g_warp == 0 && lane < kSlots && t < Tn && s0 + lane < k) {
-          float all = 0.f;
+      write_gate_grads<G>(acc, t, t < Tn, s0, k, part, dgates);
+    }
+  }
+  zero_rows(lanes_of<T, V>(dy), rows_used(offsets, N, F), F, n);
+}
+
+// ---- bf16 rows of any alignment: pairs of columns ---------------------------------------------------
+using bf16 = __nv_bfloat16;
+
+// 1 if the row's pairs on 4 bytes are the columns (2 j - 1, 2 j), 0 if (2 j, 2 j + 1).
+__device__ __forceinline__ int row_parity(const bf16* row) {
+  return static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1) & 1;
+}
+// Columns c and c + 1; those outside [0, d) read as 0 and are not written.
+__device__ __forceinline__ uint32_t load_pair(const bf16* row, int c, int d) {
+  const auto* p = reinterpret_cast<const uint16_t*>(row) + c;
+  if (c >= 0 && c + 1 < d && (reinterpret_cast<uintptr_t>(p) & 3u) == 0)
+    return __ldg(reinterpret_cast<const uint32_t*>(p));
+  const uint32_t lo = c >= 0 && c < d ? __ldg(p) : 0u, hi = c + 1 >= 0 && c + 1 < d ? __ldg(p + 1) : 0u;
+  return lo | hi << 16;
+}
+__device__ __forceinline__ void store_pair(bf16* row, int c, int d, uint32_t v) {
+  auto* p = reinterpret_cast<uint16_t*>(row) + c;
+  if (c >= 0 && c + 1 < d && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
+    __stcs(reinterpret_cast<uint32_t*>(p), v);
+    return;
+  }
+  if (c >= 0 && c < d) p[0] = static_cast<uint16_t>(v);
+  if (c + 1 >= 0 && c + 1 < d) p[1] = static_cast<uint16_t>(v >> 16);
+}
+__device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+// Pairs of a row, either way they start.
+__host__ __device__ __forceinline__ int pairs_of(int d) { return d / 2 + 1; }
+// A token's columns 2 j - 1 .. 2 j + 1, for pairs of either parity.
+struct Three {
+  uint32_t even, odd;  // (2 j, 2 j + 1), (2 j - 1, 2 j)
+  __device__ __forceinline__ void load(const bf16* row, int j, int d) {
+    even = load_pair(row, 2 * j, d);
+    const auto* p = reinterpret_cast<const uint16_t*>(row);
+    odd = (j > 0 && 2 * j - 1 < d ? __ldg(p + 2 * j - 1) : 0u) | even << 16;
+  }
+};
+
+template <int U>
+__global__ void __launch_bounds__(kThreads)
+    sort_pairs_kernel(const bf16* __restrict__ h, const int32_t* __restrict__ inv,
+                      const int32_t* __restrict__ offsets, int Tn, int d, int N, int k, bf16* __restrict__ x,
+                      int32_t* __restrict__ perm, const int32_t* status) {
+  pdl_wait();
+  pdl_trigger();
+  if (status_timed_out(status)) return;
+  const int F = Tn * k, lane = threadIdx.x & 31;
+  const int used = rows_used(offsets, N, F);
+  fill_perm(perm, used, F);
+  if (x == nullptr) return;  // the plan alone
+  RowWalk at(static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x) * kWarps,
+             (pairs_of(d) + 32 * U - 1) / (32 * U));
+  for (; at.row < Tn; at.next()) {
+    const int64_t t = at.row;
+    const int j0 = at.col * 32 * U + lane;
+    Three v[U];
 #pragma unroll
-          for (int w = 0; w < G; ++w) all += part[warp + w][lane];
-          dgates[t * k + s0 + lane] = all;
-        }
-        __syncthreads();
+    for (int u = 0; u < U; ++u) v[u].load(h + t * d, j0 + u * 32, d);
+    for (int s0 = 0; s0 < k; s0 += kSlots) {
+      const int mine = lane < kSlots ? my_row(inv, t, k, s0 + lane, F) : -1;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        const int r = __shfl_sync(0xffffffffu, mine, s);
+        if (r < 0) continue;
+        bf16* dst = x + static_cast<int64_t>(r) * d;
+        const int p = row_parity(dst);
+#pragma unroll
+        for (int u = 0; u < U; ++u) store_pair(dst, 2 * (j0 + u * 32) - p, d, p != 0 ? v[u].odd : v[u].even);
       }
     }
   }
-  zero_rows<T, V>(dy, rows_used(offsets, N, F), F, d);
+  zero_rows(reinterpret_cast<uint16_t*>(x), used, F, d);
+}
+
+template <int U>
+__global__ void __launch_bounds__(kThreads)
+    sum_pairs_kernel(const bf16* __restrict__ y, const int32_t* __restrict__ inv, const float* __restrict__ gates,
+                     int Tn, int d, int k, bf16* __restrict__ out) {
+  pdl_wait();
+  pdl_trigger();
+  const int F = Tn * k, lane = threadIdx.x & 31;
+  RowWalk at(static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x) * kWarps,
+             (pairs_of(d) + 32 * U - 1) / (32 * U));
+  for (; at.row < Tn; at.next()) {
+    const int64_t t = at.row;
+    bf16* dst = out + t * d;
+    const int parity = row_parity(dst), c0 = 2 * (at.col * 32 * U + lane) - parity;
+    float acc[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc[u][0] = acc[u][1] = 0.f;
+    for (int s0 = 0; s0 < k; s0 += kSlots) {
+      const int mine = lane < kSlots ? my_row(inv, t, k, s0 + lane, F) : -1;
+      const float my_g = lane < kSlots && s0 + lane < k && gates != nullptr ? gates[t * k + s0 + lane] : 1.f;
+      // A row whose pairs start one column off the output's is loaded from a column earlier, and a pair
+      // put together from a lane's upper half and the next lane's lower one; the last lane loads one more.
+      uint32_t raw[kSlots][U], more[kSlots];
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        const int r = __shfl_sync(0xffffffffu, mine, s);
+        const bf16* row = y + static_cast<int64_t>(r) * d;
+        const int off = row_parity(row) ^ parity;
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[s][u] = r >= 0 ? load_pair(row, c0 + u * 64 - off, d) : 0u;
+        more[s] = r >= 0 && off != 0 && lane == 31 ? load_pair(row, c0 + (U - 1) * 64 + 1, d) : 0u;
+      }
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) {
+        const int r = __shfl_sync(0xffffffffu, mine, s);
+        const float g = __shfl_sync(0xffffffffu, my_g, s);
+        if (r < 0) continue;  // (its gate may hold anything)
+        if ((row_parity(y + static_cast<int64_t>(r) * d) ^ parity) != 0) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const uint32_t first = u + 1 < U ? __shfl_sync(0xffffffffu, raw[s][u + 1 < U ? u + 1 : u], 0) : more[s];
+            uint32_t next = __shfl_down_sync(0xffffffffu, raw[s][u], 1);
+            if (lane == 31) next = first;
+            raw[s][u] = __byte_perm(raw[s][u], next, 0x5432);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          acc[u][0] = fmaf(g, low(raw[s][u]), acc[u][0]);
+          acc[u][1] = fmaf(g, high(raw[s][u]), acc[u][1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) store_pair(dst, c0 + u * 64, d, pack_bf16x2(acc[u][0], acc[u][1]));
+  }
+}
+
+template <int U, int G>
+__global__ void __launch_bounds__(kThreads)
+    unsort_backward_pairs_kernel(const bf16* __restrict__ dout, const bf16* __restrict__ y,
+                                 const float* __restrict__ gates, const int32_t* __restrict__ inv,
+                                 const int32_t* __restrict__ offsets, int Tn, int d, int N, int k,
+                                 bf16* __restrict__ dy, float* __restrict__ dgates) {
+  __shared__ float part[kWarps][kSlots];
+  pdl_wait();
+  pdl_trigger();
+  const int F = Tn * k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = pairs_of(d);
+  constexpr int kTokens = kWarps / G;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < Tn; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+    const int64_t t = t0 + warp / G;
+    if (G == 1 && t >= Tn) break;
+    for (int s0 = 0; s0 < k; s0 += kSlots) {
+      const bool own = lane < kSlots && t < Tn;
+      const int mine = own ? my_row(inv, t, k, s0 + lane, F) : -1;
+      const float my_g = own && s0 + lane < k ? gates[t * k + s0 + lane] : 0.f;
+      float acc[kSlots];
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) acc[s] = 0.f;
+      if (t < Tn)
+        for (int j0 = warp % G * 32 * U + lane; j0 - lane < n; j0 += G * 32 * U) {
+          uint32_t raw[kSlots][U];
+          Three v[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) v[u].load(dout + t * d, j0 + u * 32, d);
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s) {
+            const int r = __shfl_sync(0xffffffffu, mine, s);
+            const bf16* row = y + static_cast<int64_t>(r) * d;
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[s][u] = r >= 0 ? load_pair(row, 2 * (j0 + u * 32) - row_parity(row), d) : 0u;
+          }
+#pragma unroll
+          for (int s = 0; s < kSlots; ++s) {
+            const int r = __shfl_sync(0xffffffffu, mine, s);
+            const float g = __shfl_sync(0xffffffffu, my_g, s);
+            if (r < 0) continue;
+            const int p = row_parity(y + static_cast<int64_t>(r) * d);
+            bf16* dst = dy + static_cast<int64_t>(r) * d;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const uint32_t a = p != 0 ? v[u].odd : v[u].even;
+              acc[s] = fmaf(low(a), low(raw[s][u]), acc[s]);
+              acc[s] = fmaf(high(a), high(raw[s][u]), acc[s]);
+              store_pair(dst, 2 * (j0 + u * 32) - p, d, pack_bf16x2(g * low(a), g * high(a)));
+            }
+          }
+        }
+      write_gate_grads<G>(acc, t, t < Tn, s0, k, part, dgates);
+    }
+  }
+  zero_rows(reinterpret_cast<uint16_t*>(dy), rows_used(offsets, N, F), F, d);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
@@ -281,52 +580,79 @@ bool vectors(const TokenArgs& a, int es) {
   return (all & 15u) == 0 && static_cast<int64_t>(a.d) * es % 16 == 0;
 }
 
+dim3 item_grid(int64_t rows, int units, int U, int num_sms) {
+  return dim3(blocks_for(rows * ((units + 32 * U - 1) / (32 * U)), kWarps, num_sms, 16));
+}
+
 template <typename T, int V, int U>
 cudaError_t sort_rows(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  const int64_t items = a.dst != nullptr ? a.T * ((a.d / V + 32 * U - 1) / (32 * U)) : (a.T * a.k + 255) / 256;
-  return launch_pdl(sort_kernel<T, V, U>, dim3(blocks_for(items, kWarps, num_sms, 16)), dim3(kThreads), 0, st, 1,
-                    static_cast<const T*>(a.src), a.inv, a.offsets, static_cast<int>(a.T), a.d, a.N, a.k,
-                    static_cast<T*>(a.dst), a.perm, a.status);
+  const dim3 grid = a.dst != nullptr ? item_grid(a.T, a.d / V, U, num_sms)
+                                     : dim3(blocks_for(a.T * a.k, kThreads, num_sms, 16));
+  return launch_pdl(sort_kernel<T, V, U>, grid, dim3(kThreads), 0, st, 1, static_cast<const T*>(a.src), a.inv,
+                    a.offsets, static_cast<int>(a.T), a.d, a.N, a.k, static_cast<T*>(a.dst), a.perm, a.status);
 }
 template <typename T, int V, int U>
 cudaError_t sum_rows(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  const int64_t items = a.T * ((a.d / V + 32 * U - 1) / (32 * U));
-  return launch_pdl(sum_kernel<T, V, U>, dim3(blocks_for(items, kWarps, num_sms, 16)), dim3(kThreads), 0, st, 1,
+  return launch_pdl(sum_kernel<T, V, U>, item_grid(a.T, a.d / V, U, num_sms), dim3(kThreads), 0, st, 1,
                     static_cast<const T*>(a.src), a.inv, a.gates, static_cast<int>(a.T), a.d, a.k,
                     static_cast<T*>(a.dst));
 }
-template <typename T, int V, int U, int G>
-cudaError_t unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  return launch_pdl(unsort_backward_kernel<T, V, U, G>, dim3(blocks_for(a.T, kWarps / G, num_sms, 16)),
-                    dim3(kThreads), 0, st, 1, static_cast<const T*>(a.src), static_cast<const T*>(a.y), a.gates,
-                    a.inv, a.offsets, static_cast<int>(a.T), a.d, a.N, a.k, static_cast<T*>(a.dst), a.dgates);
-}
-template <typename T, int V, int U>
-cudaError_t unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  // a warp a token while that fills the SMs, else a block a token
-  return a.T >= static_cast<int64_t>(num_sms) * 16 ? unsort_backward<T, V, U, 1>(a, num_sms, st)
-                                                   : unsort_backward<T, V, U, kWarps>(a, num_sms, st);
+
+// unsort_backward: a warp a token while that fills the SMs, else a block a token.
+template <typename T>
+cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
+                                                 int, int, int, T*, float*),
+                                   void (*blocks)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
+                                                  int, int, int, T*, float*),
+                                   const TokenArgs& a, int num_sms, cudaStream_t st) {
+  const bool many = a.T >= static_cast<int64_t>(num_sms) * 16;
+  return launch_pdl(many ? warps : blocks, dim3(blocks_for(a.T, many ? kWarps : 1, num_sms, 16)), dim3(kThreads), 0, st,
+                    1, static_cast<const T*>(a.src), static_cast<const T*>(a.y), a.gates, a.inv, a.offsets,
+                    static_cast<int>(a.T), a.d, a.N, a.k, static_cast<T*>(a.dst), a.dgates);
 }
 
 }  // namespace
 
+cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm,
+                              int32_t* inv, int32_t* status, cudaStream_t st) {
+  int blocks = 1;
+  while (blocks * kPlanThreads < F) blocks *= 2;
+  const size_t smem = sizeof(int) * static_cast<size_t>(N) * (32 + kPlanBlocks + 1);
+  static_assert(sizeof(int) * kMaxExperts * (32 + kPlanBlocks + 1) + 1024 <= 48 * 1024, "no opt-in needed");
+  return launch_pdl(plan_kernel, dim3(blocks), dim3(kPlanThreads), smem, st, blocks, idx, F, k, N, blocks, offsets,
+                    perm, inv, status);
+}
+
 cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  if (a.bf16)
-    return vectors(a, 2) ? sort_rows<__nv_bfloat16, 8, 2>(a, num_sms, st)
-                         : sort_rows<__nv_bfloat16, 1, 8>(a, num_sms, st);
-  return vectors(a, 4) ? sort_rows<float, 4, 2>(a, num_sms, st) : sort_rows<float, 1, 8>(a, num_sms, st);
+  if (!a.bf16) return vectors(a, 4) ? sort_rows<float, 4, 2>(a, num_sms, st) : sort_rows<float, 1, 8>(a, num_sms, st);
+  if (vectors(a, 2)) return sort_rows<bf16, 8, 2>(a, num_sms, st);
+  constexpr int U = 4;
+  const dim3 grid = a.dst != nullptr ? item_grid(a.T, pairs_of(a.d), U, num_sms)
+                                     : dim3(blocks_for(a.T * a.k, kThreads, num_sms, 16));
+  return launch_pdl(sort_pairs_kernel<U>, grid, dim3(kThreads), 0, st, 1, static_cast<const bf16*>(a.src), a.inv, a.offsets, static_cast<int>(a.T), a.d, a.N, a.k,
+                    static_cast<bf16*>(a.dst), a.perm, a.status);
 }
 cudaError_t launch_token_sum(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  if (a.bf16)
-    return vectors(a, 2) ? sum_rows<__nv_bfloat16, 8, 1>(a, num_sms, st)
-                         : sum_rows<__nv_bfloat16, 1, 4>(a, num_sms, st);
-  return vectors(a, 4) ? sum_rows<float, 4, 1>(a, num_sms, st) : sum_rows<float, 1, 4>(a, num_sms, st);
+  if (!a.bf16) return vectors(a, 4) ? sum_rows<float, 4, 1>(a, num_sms, st) : sum_rows<float, 1, 2>(a, num_sms, st);
+  if (vectors(a, 2)) return sum_rows<bf16, 8, 1>(a, num_sms, st);
+  // four pairs a lane unless that leaves most lanes of a narrow row without one (k = 8, d = 2047: 57 us
+  // with four, 68 with two; k = 2, d = 65: 21 and 14)
+  const bool wide = pairs_of(a.d) > 64;
+  return launch_pdl(wide ? sum_pairs_kernel<4> : sum_pairs_kernel<2>,
+                    item_grid(a.T, pairs_of(a.d), wide ? 4 : 2, num_sms), dim3(kThreads), 0, st, 1,
+                    static_cast<const bf16*>(a.src), a.inv, a.gates, static_cast<int>(a.T), a.d, a.k,
+                    static_cast<bf16*>(a.dst));
 }
 cudaError_t launch_token_unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st) {
-  if (a.bf16)
-    return vectors(a, 2) ? unsort_backward<__nv_bfloat16, 8, 1>(a, num_sms, st)
-                         : unsort_backward<__nv_bfloat16, 1, 4>(a, num_sms, st);
-  return vectors(a, 4) ? unsort_backward<float, 4, 1>(a, num_sms, st) : unsort_backward<float, 1, 4>(a, num_sms, st);
+  if (!a.bf16)
+    return vectors(a, 4) ? launch_unsort_backward<float>(unsort_backward_kernel<float, 4, 1, 1>,
+                                                         unsort_backward_kernel<float, 4, 1, kWarps>, a, num_sms, st)
+                         : launch_unsort_backward<float>(unsort_backward_kernel<float, 1, 2, 1>,
+                                                         unsort_backward_kernel<float, 1, 2, kWarps>, a, num_sms, st);
+  return vectors(a, 2) ? launch_unsort_backward<bf16>(unsort_backward_kernel<bf16, 8, 1, 1>,
+                                                      unsort_backward_kernel<bf16, 8, 1, kWarps>, a, num_sms, st)
+                       : launch_unsort_backward<bf16>(unsort_backward_pairs_kernel<2, 1>,
+                                                      unsort_backward_pairs_kernel<2, kWarps>, a, num_sms, st);
 }
 
 }  // namespace pr2
