@@ -259,7 +259,7 @@ struct TokenArgs {
   const int32_t* status;   // sort: of the dispatch before it (nullable)
 };
 // The plan of F <= kPlanSlots slots, perm's tail included (status nullable).
-constexpr int kPlanSlots = 8192;
+constexpr int kPlanSlots = 16384;
 cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm,
                               int32_t* inv, int32_t* status, cudaStream_t st);
 cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st);

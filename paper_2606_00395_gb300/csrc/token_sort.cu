@@ -7,7 +7,7 @@
 // order are found through inv, so nothing is written twice and the sums do not depend on the launch
 // but for the split of a row over warps.  Rows past offsets[N], which no slot names, are zeroed.
 // A row number outside [0, T k) is taken as an invalid slot.
-// The plan of up to 8192 slots is made by one cluster (plan_kernel), of more by the layer forward's
+// The plan of up to 16384 slots is made by one cluster (plan_kernel), of more by the layer forward's
 // dispatch.
 //
 // All of it is bound by HBM: the k expert rows, read or written once.  A warp takes a piece of a
@@ -109,42 +109,56 @@ __device__ __forceinline__ void fill_perm(int32_t* __restrict__ perm, int from, 
 }
 
 // ---- the plan of a batch of up to kPlanSlots slots -----------------------------------------------------
-// One cluster, a slot per thread: counts per warp and expert by __match_any_sync, summed per block, the
-// blocks' counts exchanged through distributed shared memory; then every block scans the experts'
-// totals and places its slots in order.  No memory outside the cluster is waited for, so it is an
-// ordinary launch.  Latency-bound: 2048 slots of 128 experts take about 4 us where the dispatch's
-// cooperative launch and the clearing of its counters take 9.
+// One cluster, S slots per thread (a thread's are 1024 apart): counts per 32 slots and expert by
+// __match_any_sync, summed per block, the blocks' counts exchanged through distributed shared memory;
+// then every block scans the experts' totals and places its slots in order.  No memory outside the
+// cluster is waited for, so it is an ordinary launch.  Latency-bound: with k = 8 and 128 experts 2048 and
+// 8192 slots take 5.4 us a call (dispatch: 12 us), 16384 slots 7.6, and 32768 with four slots a thread 12.3,
+// where the dispatch's many blocks take 14 and leave no single cluster in front of the rows.
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanBlocks = 8;
-static_assert(kPlanThreads * kPlanBlocks == kPlanSlots, "a slot per thread");
+constexpr int kPlanMost = 2;  // slots per thread
+static_assert(kPlanThreads * kPlanBlocks * kPlanMost == kPlanSlots, "slots of one cluster");
 
+constexpr size_t plan_smem_bytes(int N, int S) { return sizeof(int) * static_cast<size_t>(N) * (32 * S + kPlanBlocks + 1); }
+
+template <int S>
 __global__ void __launch_bounds__(kPlanThreads)
     plan_kernel(const int32_t* __restrict__ idx, int F, int k, int N, int blocks, int32_t* __restrict__ offsets,
                 int32_t* __restrict__ perm, int32_t* __restrict__ inv, int32_t* __restrict__ status) {
   extern __shared__ int plan_smem[];
-  int* before = plan_smem;                        // [32][N] slots of the expert in earlier warps
-  int* counts = before + 32 * N;                  // [kPlanBlocks][N]
-  int* first = counts + kPlanBlocks * N;          // [N] row of the block's first slot of the expert
+  int* before = plan_smem;                // [32 S][N] slots of the expert in earlier groups of 32
+  int* counts = before + 32 * S * N;      // [kPlanBlocks][N]
+  int* first = counts + kPlanBlocks * N;  // [N] row of the block's first slot of the expert
   __shared__ int warp_sum[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = blocks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  for (int i = tid; i < 32 * N; i += kPlanThreads) before[i] = 0;
+  for (int i = tid; i < 32 * S * N; i += kPlanThreads) before[i] = 0;
   if (blocks > 1) cluster_sync();  // peers write to counts
   pdl_wait();
   pdl_trigger();
-  const int f = rank * kPlanThreads + tid;
-  int e = f < F ? idx[f] : -1;
-  if (e < 0 || e >= N) e = -1;
-  for (int g = f - f % k; g < f && e >= 0; ++g)
-    if (idx[g] == e) e = -1;  // repeated within its token
-  if (f < F && e < 0 && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
+  const int f0 = rank * kPlanThreads * S + tid;
+  int e[S];
+  unsigned same[S];
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int f = f0 + i * kPlanThreads;
+    e[i] = f < F ? idx[f] : -1;
+    if (e[i] < 0 || e[i] >= N) e[i] = -1;
+    for (int g = f - f % k; g < f && e[i] >= 0; ++g)
+      if (idx[g] == e[i]) e[i] = -1;  // repeated within its token
+    if (f < F && e[i] < 0 && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
+    same[i] = __match_any_sync(0xffffffffu, e[i]);
+  }
   __syncthreads();
-  const unsigned same = __match_any_sync(0xffffffffu, e);
-  if (e >= 0 && lane == __ffs(same) - 1) before[warp * N + e] = __popc(same);
+#pragma unroll
+  for (int i = 0; i < S; ++i)
+    if (e[i] >= 0 && lane == __ffs(same[i]) - 1) before[(i * 32 + warp) * N + e[i]] = __popc(same[i]);
   __syncthreads();
   if (tid < N) {
     int sum = 0;
-    for (int w = 0; w < 32; ++w) {
+#pragma unroll 8
+    for (int w = 0; w < 32 * S; ++w) {
       const int c = before[w * N + tid];
       before[w * N + tid] = sum;
       sum += c;
@@ -188,14 +202,33 @@ __global__ void __launch_bounds__(kPlanThreads)
   }
   if (rank == 0 && tid == 0) offsets[N] = used;
   __syncthreads();
-  if (f >= F) return;
-  int row = -1;
-  if (e >= 0) {
-    row = first[e] + before[warp * N + e] + __popc(same & lanemask_lt());
-    perm[row] = f;
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int f = f0 + i * kPlanThreads;
+    if (f >= F) break;
+    int row = -1;
+    if (e[i] >= 0) {
+      row = first[e[i]] + before[(i * 32 + warp) * N + e[i]] + __popc(same[i] & lanemask_lt());
+      perm[row] = f;
+    }
+    inv[f] = row;
+    if (f >= used) perm[f] = -1;
   }
-  inv[f] = row;
-  if (f >= used) perm[f] = -1;
+}
+
+template <int S>
+cudaError_t run_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm, int32_t* inv,
+                     int32_t* status, cudaStream_t st) {
+  int blocks = 1;
+  while (blocks * kPlanThreads * S < F) blocks *= 2;
+  constexpr size_t most = plan_smem_bytes(kMaxExperts, S);  // the kernel's limit, whatever N
+  if (most + 1024 > 48 * 1024) {
+    const cudaError_t err = cudaFuncSetAttribute(plan_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 static_cast<int>(most));
+    if (err != cudaSuccess) return err;
+  }
+  return launch_pdl(plan_kernel<S>, dim3(blocks), dim3(kPlanThreads), plan_smem_bytes(N, S), st, blocks, idx, F, k, N,
+                    blocks, offsets, perm, inv, status);
 }
 
 // ---- sort: a warp per (token, U lanes' worth of its columns) ---------------------------------------
@@ -615,12 +648,8 @@ cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float
 
 cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm,
                               int32_t* inv, int32_t* status, cudaStream_t st) {
-  int blocks = 1;
-  while (blocks * kPlanThreads < F) blocks *= 2;
-  const size_t smem = sizeof(int) * static_cast<size_t>(N) * (32 + kPlanBlocks + 1);
-  static_assert(sizeof(int) * kMaxExperts * (32 + kPlanBlocks + 1) + 1024 <= 48 * 1024, "no opt-in needed");
-  return launch_pdl(plan_kernel, dim3(blocks), dim3(kPlanThreads), smem, st, blocks, idx, F, k, N, blocks, offsets,
-                    perm, inv, status);
+  if (F <= kPlanThreads * kPlanBlocks) return run_plan<1>(idx, F, k, N, offsets, perm, inv, status, st);
+  return run_plan<kPlanMost>(idx, F, k, N, offsets, perm, inv, status, st);
 }
 
 cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st) {

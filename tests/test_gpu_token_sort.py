@@ -16,7 +16,7 @@ DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 EPS = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}  # half a unit in the last place
 SHAPES = [  # T, d, N, k
     (1, 1, 1, 1), (1, 7168, 256, 8), (2, 9, 3, 2), (5, 64, 8, 8), (33, 130, 60, 4), (128, 1024, 128, 8),
-    (129, 1023, 6, 6), (300, 257, 40, 32), (700, 2048, 128, 8), (1500, 40, 256, 3), (40, 8200, 16, 2),
+    (129, 1023, 6, 6), (300, 257, 40, 32), (700, 2048, 128, 8), (1500, 40, 256, 3), (40, 8200, 16, 2), (1500, 9, 250, 8), (4000, 16, 256, 8), (4097, 8, 64, 8), (9000, 4, 7, 3),
     (17, 1028, 16, 5), (9, 20001, 16, 5)]
 
 
