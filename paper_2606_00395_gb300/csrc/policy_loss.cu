@@ -191,6 +191,14 @@ __device__ __noinline__ RowSum add_careful(RowSum s, const uint4* src, int v, in
   return s;
 }
 
+// y, or if it is lower a power far below 2^-126 (so that an entry of -inf gives 0 in both sums); a NaN
+// stays one.
+__device__ __forceinline__ float at_least(float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(y), "f"(-16384.f));
+  return r;
+}
+
 // The two sums over 16 entries relative to M, in the order of pairs.
 template <typename T>
 __device__ __forceinline__ void sum_16(const uint4 (&raw)[16 / Vec<T>::kElems], float M, float scale, float& l,
@@ -204,12 +212,13 @@ __device__ __forceinline__ void sum_16(const uint4 (&raw)[16 / Vec<T>::kElems], 
     Vec<T>::pairs(raw[j], z);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-      const uint64_t y2 = fma2(z[i], scale2, ref2);
       float a, b;
-      unpack2(y2, a, b);
+      unpack2(fma2(z[i], scale2, ref2), a, b);
+      a = at_least(a);
+      b = at_least(b);
       const uint64_t p2 = pack2(exp2_approx(a), exp2_approx(b));
       l2 = add2(l2, p2);
-      e2 = fma2(p2, y2, e2);
+      e2 = fma2(p2, pack2(a, b), e2);
     }
   }
   float a, b;
@@ -221,15 +230,15 @@ __device__ __forceinline__ void sum_16(const uint4 (&raw)[16 / Vec<T>::kElems], 
 
 // 16 entries, the vectors src[v], src[v + stride], ... which are in raw.  They are summed relative to
 // s.m as it is; where that does not do (M is NaN, the sum is too large for it or so small that entries
-// that matter may have vanished, an entry of -inf made 0 inf of the second sum, an entry is NaN) they
-// go the careful way.  M: scaled_ref(s.m), kept by the caller.
+// that matter may have vanished, an entry is NaN) they go the careful way.  M: scaled_ref(s.m), kept by
+// the caller.
 template <typename T>
 __device__ __forceinline__ void add_vectors(RowSum& s, float& M, const uint4 (&raw)[16 / Vec<T>::kElems],
                                             const uint4* src, int v, int stride, int n, float scale) {
   constexpr float kMost = 1.0995116e12f, kLeast = 8.6736174e-19f;  // 2^40, 2^-60
   float l, e;
   sum_16<T>(raw, M, scale, l, e);
-  if (l > kLeast && fmaf(e, 0.f, l) < kMost) {
+  if (l > kLeast && l < kMost) {
     s.l += l;
     s.e += e;
   } else {
@@ -915,9 +924,11 @@ cudaError_t launch(const PolicyArgs& a, int num_sms, cudaStream_t st) {
           : nvec <= 256 ? launch_pdl(policy_warp_kernel<T, 8>, grid, dim3(kThreads), 0, st, 1, a)
                       : launch_pdl(policy_warp_kernel<T, 16>, grid, dim3(kThreads), 0, st, 1, a);
   } else {
-    // A row that does not fit the rings is read again from L2: the rows in flight have to stay there
-    // (with the gradients on their way, 48 of its 129 MB).  A wider cluster too while that puts idle CTAs to work and leaves every
-    // thread two vectors.
+    // CTAs a row.  A row that does not fit the rings is read again from L2, so the rows in flight have to
+    // stay there (with the gradients on their way, 48 of its 129 MB): 4096 bf16 rows of 65536 take 220 us
+    // with one CTA a row, 204 with two.  No more than that, because a round's exchange of the sums takes
+    // its time however small the slices are (rows of 131072: 397 us with four, 510 with eight).  A wider
+    // cluster too while that puts idle CTAs to work and leaves every thread four vectors.
     int C = 1;
     if (a.grad != nullptr)
       while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * kRingBytes) &&
