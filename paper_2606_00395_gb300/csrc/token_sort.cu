@@ -631,14 +631,16 @@ cudaError_t sum_rows(const TokenArgs& a, int num_sms, cudaStream_t st) {
                     static_cast<T*>(a.dst));
 }
 
-// unsort_backward: a warp a token while that fills the SMs, else a block a token.
+// unsort_backward: a block a token for few tokens, and for rows of a piece or more a warp while a warp a
+// token would leave the SMs unevenly filled; else a warp a token (bf16, k = 8, us with a warp / a block:
+// 4096 x 2048 60.2 / 47.3, 8192 x 7168 341 / 321, 32768 x 2048 351 / 374, 4096 x 512 14.0 / 26.1).
 template <typename T>
 cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
                                                  int, int, int, T*, float*),
                                    void (*blocks)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
                                                   int, int, int, T*, float*),
-                                   const TokenArgs& a, int num_sms, cudaStream_t st) {
-  const bool many = a.T >= static_cast<int64_t>(num_sms) * 16;
+                                   int pieces, const TokenArgs& a, int num_sms, cudaStream_t st) {
+  const bool many = a.T >= static_cast<int64_t>(num_sms) * (pieces >= kWarps ? 64 : 2);
   return launch_pdl(many ? warps : blocks, dim3(blocks_for(a.T, many ? kWarps : 1, num_sms, 16)), dim3(kThreads), 0, st,
                     1, static_cast<const T*>(a.src), static_cast<const T*>(a.y), a.gates, a.inv, a.offsets,
                     static_cast<int>(a.T), a.d, a.N, a.k, static_cast<T*>(a.dst), a.dgates);
@@ -675,13 +677,16 @@ cudaError_t launch_token_sum(const TokenArgs& a, int num_sms, cudaStream_t st) {
 cudaError_t launch_token_unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st) {
   if (!a.bf16)
     return vectors(a, 4) ? launch_unsort_backward<float>(unsort_backward_kernel<float, 4, 1, 1>,
-                                                         unsort_backward_kernel<float, 4, 1, kWarps>, a, num_sms, st)
+                                                         unsort_backward_kernel<float, 4, 1, kWarps>, a.d / 128, a,
+                                                         num_sms, st)
                          : launch_unsort_backward<float>(unsort_backward_kernel<float, 1, 2, 1>,
-                                                         unsort_backward_kernel<float, 1, 2, kWarps>, a, num_sms, st);
+                                                         unsort_backward_kernel<float, 1, 2, kWarps>, a.d / 64, a,
+                                                         num_sms, st);
   return vectors(a, 2) ? launch_unsort_backward<bf16>(unsort_backward_kernel<bf16, 8, 1, 1>,
-                                                      unsort_backward_kernel<bf16, 8, 1, kWarps>, a, num_sms, st)
+                                                      unsort_backward_kernel<bf16, 8, 1, kWarps>, a.d / 256, a,
+                                                      num_sms, st)
                        : launch_unsort_backward<bf16>(unsort_backward_pairs_kernel<2, 1>,
-                                                      unsort_backward_pairs_kernel<2, kWarps>, a, num_sms, st);
+                                                      unsort_backward_pairs_kernel<2, kWarps>, a.d / 128, a, num_sms, st);
 }
 
 }  // namespace pr2
