@@ -193,8 +193,9 @@ pr2_status pr2_token_sort(const pr2_dims* dims, const void* h, const int32_t* id
   a.src = h;
   a.dst = x;
   if (idx != nullptr && dm.T * dm.k <= kPlanSlots) {
-    const cudaError_t err = launch_token_plan(idx, static_cast<int>(dm.T * dm.k), dm.k, dm.N, offsets,
-                                              perm, inv, status_dev, st);
+    const PlanWorkspace w = carve_plan(dm, static_cast<uint8_t*>(workspace));
+    const cudaError_t err = launch_token_plan(idx, static_cast<int>(dm.T * dm.k), dm.k, dm.N, w.blk_hist,
+                                              offsets, perm, inv, status_dev, st);
     if (err != cudaSuccess || x == nullptr) return finish(err, dm.flags, status_dev, st);
   } else if (idx != nullptr) {
     const PlanWorkspace w = carve_plan(dm, static_cast<uint8_t*>(workspace));

@@ -258,10 +258,11 @@ struct TokenArgs {
   float* dgates;           // unsort_backward
   const int32_t* status;   // sort: of the dispatch before it (nullable)
 };
-// The plan of F <= kPlanSlots slots, perm's tail included (status nullable).
-constexpr int kPlanSlots = 16384;
-cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm,
-                              int32_t* inv, int32_t* status, cudaStream_t st);
+// The plan of F <= kPlanSlots slots, perm's tail included (status nullable; hist: a block histogram as
+// the dispatch's, [F / kDispatchChunk][N]).
+constexpr int kPlanSlots = 1 << 22;
+cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* hist, int32_t* offsets,
+                              int32_t* perm, int32_t* inv, int32_t* status, cudaStream_t st);
 cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_token_sum(const TokenArgs& a, int num_sms, cudaStream_t st);  // gates nullable
 cudaError_t launch_token_unsort_backward(const TokenArgs& a, int num_sms, cudaStream_t st);

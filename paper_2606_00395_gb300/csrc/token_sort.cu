@@ -7,8 +7,8 @@
 // order are found through inv, so nothing is written twice and the sums do not depend on the launch
 // but for the split of a row over warps.  Rows past offsets[N], which no slot names, are zeroed.
 // A row number outside [0, T k) is taken as an invalid slot.
-// The plan of up to 16384 slots is made by one cluster (plan_kernel), of more by the layer forward's
-// dispatch.
+// The plan of up to 32768 slots is made by one cluster (plan_kernel), of up to 4 M slots by two launches
+// (plan_count_kernel, plan_place_kernel), of more by the layer forward's dispatch.
 //
 // All of it is bound by HBM: the k expert rows, read or written once.  A warp takes a piece of a
 // token's row, a lane V neighbouring columns: 16 bytes where d and the pointers allow it, else one
@@ -110,17 +110,68 @@ __device__ __forceinline__ void fill_perm(int32_t* __restrict__ perm, int from, 
 
 // ---- the plan of a batch of up to kPlanSlots slots -----------------------------------------------------
 // One cluster, S slots per thread (a thread's are 1024 apart): counts per 32 slots and expert by
-// __match_any_sync, summed per block, the blocks' counts exchanged through distributed shared memory;
+// ballots, summed per block, the blocks' counts exchanged through distributed shared memory;
 // then every block scans the experts' totals and places its slots in order.  No memory outside the
-// cluster is waited for, so it is an ordinary launch.  Latency-bound: with k = 8 and 128 experts 2048 and
-// 8192 slots take 5.4 us a call (dispatch: 12 us), 16384 slots 7.6, and 32768 with four slots a thread 12.3,
-// where the dispatch's many blocks take 14 and leave no single cluster in front of the rows.
+// cluster is waited for, so it is an ordinary launch.  Latency-bound: with k = 8 and 128 experts up to
+// 8192 slots take 5.2 us a call, 16384 (two a thread) 5.9 and 32768 (four) 9.3, where the dispatch's
+// cooperative launch and the clearing of its counters take 12 to 14 and the two launches below 12.0.
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanBlocks = 8;
-constexpr int kPlanMost = 2;  // slots per thread
-static_assert(kPlanThreads * kPlanBlocks * kPlanMost == kPlanSlots, "slots of one cluster");
 
 constexpr size_t plan_smem_bytes(int N, int S) { return sizeof(int) * static_cast<size_t>(N) * (32 * S + kPlanBlocks + 1); }
+
+// The lanes with the same e (-1 <= e < N) as this one: a ballot per bit, which takes less than a
+// __match_any_sync (placing 4096 slots of a block 1 us less, counting them so 3 us).
+__device__ __forceinline__ unsigned lanes_with(int e, int N) {
+  unsigned same = __ballot_sync(0xffffffffu, e >= 0);
+  if (e < 0) same = ~same;
+  for (int bits = N - 1, b = 0; bits > 0; bits >>= 1, ++b) {
+    const unsigned m = __ballot_sync(0xffffffffu, (e >> b) & 1);
+    same &= (e >> b) & 1 ? m : ~m;
+  }
+  return same;
+}
+
+// Exclusive scan, from `sum` on, of column[0], column[stride], ... (kRows of them); returns the end.
+// Sixteen are loaded before any is stored.
+template <int kRows>
+__device__ __forceinline__ int scan_column(int* column, int stride, int sum) {
+#pragma unroll 1
+  for (int w = 0; w < kRows; w += 16) {
+    int c[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) c[j] = column[(w + j) * stride];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      column[(w + j) * stride] = sum;
+      sum += c[j];
+    }
+  }
+  return sum;
+}
+
+// The thread's slots f0 + i 1024: their expert, -1 if invalid.  A slot's earlier ones in its token are
+// the lanes below it, or in the warp before.
+template <int S>
+__device__ __forceinline__ void slots_of(const int32_t* __restrict__ idx, int f0, int F, int k, int N, int (&e)[S],
+                                         int32_t* __restrict__ status) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < S; ++i) e[i] = f0 + i * kPlanThreads < F ? idx[f0 + i * kPlanThreads] : -1;
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    const int f = f0 + i * kPlanThreads, slot = f % k, raw = e[i];
+    bool bad = raw < 0 || raw >= N;
+    for (int j = 1; j < k; ++j) {
+      const int other = __shfl_up_sync(0xffffffffu, raw, j);
+      bad |= j <= slot && j <= lane && other == raw;
+    }
+    if (f < F)
+      for (int j = lane + 1; j <= slot; ++j) bad |= idx[f - j] == raw;
+    if (f < F && bad && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
+    e[i] = bad ? -1 : raw;
+  }
+}
 
 template <int S>
 __global__ void __launch_bounds__(kPlanThreads)
@@ -140,29 +191,16 @@ __global__ void __launch_bounds__(kPlanThreads)
   const int f0 = rank * kPlanThreads * S + tid;
   int e[S];
   unsigned same[S];
+  slots_of(idx, f0, F, k, N, e, status);
 #pragma unroll
-  for (int i = 0; i < S; ++i) {
-    const int f = f0 + i * kPlanThreads;
-    e[i] = f < F ? idx[f] : -1;
-    if (e[i] < 0 || e[i] >= N) e[i] = -1;
-    for (int g = f - f % k; g < f && e[i] >= 0; ++g)
-      if (idx[g] == e[i]) e[i] = -1;  // repeated within its token
-    if (f < F && e[i] < 0 && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
-    same[i] = __match_any_sync(0xffffffffu, e[i]);
-  }
+  for (int i = 0; i < S; ++i) same[i] = lanes_with(e[i], N);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < S; ++i)
     if (e[i] >= 0 && lane == __ffs(same[i]) - 1) before[(i * 32 + warp) * N + e[i]] = __popc(same[i]);
   __syncthreads();
   if (tid < N) {
-    int sum = 0;
-#pragma unroll 8
-    for (int w = 0; w < 32 * S; ++w) {
-      const int c = before[w * N + tid];
-      before[w * N + tid] = sum;
-      sum += c;
-    }
+    const int sum = scan_column<32 * S>(before + tid, N, 0);
     for (int b = 0; b < blocks; ++b) {
       const uint32_t at = smem_u32(&counts[rank * N + tid]);
       if (blocks > 1)
@@ -209,6 +247,101 @@ __global__ void __launch_bounds__(kPlanThreads)
     int row = -1;
     if (e[i] >= 0) {
       row = first[e[i]] + before[(i * 32 + warp) * N + e[i]] + __popc(same[i] & lanemask_lt());
+      perm[row] = f;
+    }
+    inv[f] = row;
+    if (f >= used) perm[f] = -1;
+  }
+}
+
+// ---- the plan of larger batches -------------------------------------------------------------------------
+// Blocks of kLargeSlots slots: one launch counts each block's slots per expert, the next adds up all
+// blocks' counts, and the earlier blocks' apart, and places its own.  T = 32768, k = 8, N = 128: 12.7 us a
+// call, the dispatch's one cooperative launch with a grid barrier 21.
+constexpr int kLargeMost = 4;  // slots per thread
+constexpr int kLargeSlots = kPlanThreads * kLargeMost;
+
+__global__ void __launch_bounds__(kPlanThreads)
+    plan_count_kernel(const int32_t* __restrict__ idx, int F, int k, int N, int32_t* __restrict__ hist,
+                      int32_t* __restrict__ status) {
+  __shared__ int sum[kMaxExperts];
+  if (threadIdx.x < kMaxExperts) sum[threadIdx.x] = 0;
+  pdl_wait();
+  pdl_trigger();
+  __syncthreads();
+  int e[kLargeMost];
+  slots_of(idx, static_cast<int>(blockIdx.x) * kLargeSlots + static_cast<int>(threadIdx.x), F, k, N, e, status);
+#pragma unroll
+  for (int i = 0; i < kLargeMost; ++i)
+    if (e[i] >= 0) atomicAdd(&sum[e[i]], 1);
+  __syncthreads();
+  if (static_cast<int>(threadIdx.x) < N) hist[static_cast<int64_t>(blockIdx.x) * N + threadIdx.x] = sum[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+    plan_place_kernel(const int32_t* __restrict__ idx, int F, int k, int N, const int32_t* __restrict__ hist,
+                      int32_t* __restrict__ offsets, int32_t* __restrict__ perm, int32_t* __restrict__ inv) {
+  extern __shared__ int plan_smem[];
+  int* before = plan_smem;                        // [32 kLargeMost][N]
+  int* total = before + 32 * kLargeMost * N;      // [N] slots of the expert in all blocks
+  int* earlier = total + N;                       // [N] in earlier blocks; then the row of the block's first
+  __shared__ int warp_sum[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x, blocks = gridDim.x;
+  for (int i = tid; i < (32 * kLargeMost + 2) * N; i += kPlanThreads) before[i] = 0;
+  pdl_wait();
+  pdl_trigger();
+  const int f0 = rank * kLargeSlots + tid;
+  int e[kLargeMost];
+  unsigned same[kLargeMost];
+  slots_of(idx, f0, F, k, N, e, nullptr);
+#pragma unroll
+  for (int i = 0; i < kLargeMost; ++i) same[i] = lanes_with(e[i], N);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kLargeMost; ++i)
+    if (e[i] >= 0 && lane == __ffs(same[i]) - 1) before[(i * 32 + warp) * N + e[i]] = __popc(same[i]);
+  // blocks' counts: thread (p, n) takes expert n of every parts-th block
+  const int parts = kPlanThreads / N, p = tid / N, n = tid - p * N;
+  if (p < parts) {
+    int all = 0, mine = 0;
+#pragma unroll 4
+    for (int b = p; b < blocks; b += parts) {
+      const int c = hist[static_cast<int64_t>(b) * N + n];
+      all += c;
+      mine += b < rank ? c : 0;
+    }
+    atomicAdd(&total[n], all);
+    atomicAdd(&earlier[n], mine);
+  }
+  __syncthreads();
+  const int all = tid < N ? total[tid] : 0;
+  int scan = all;  // inclusive over the experts
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_sum[warp] = scan;
+  __syncthreads();
+  int below = 0, used = 0;
+  for (int w = 0; w < kMaxExperts / 32; ++w) {
+    below += w < warp ? warp_sum[w] : 0;
+    used += warp_sum[w];
+  }
+  if (tid < N) {
+    const int off = below + scan - all;
+    if (rank == 0) offsets[tid] = off;
+    scan_column<32 * kLargeMost>(before + tid, N, off + earlier[tid]);
+  }
+  if (rank == 0 && tid == 0) offsets[N] = used;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kLargeMost; ++i) {
+    const int f = f0 + i * kPlanThreads;
+    if (f >= F) break;
+    int row = -1;
+    if (e[i] >= 0) {
+      row = before[(i * 32 + warp) * N + e[i]] + __popc(same[i] & lanemask_lt());
       perm[row] = f;
     }
     inv[f] = row;
@@ -648,10 +781,20 @@ cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float
 
 }  // namespace
 
-cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* offsets, int32_t* perm,
-                              int32_t* inv, int32_t* status, cudaStream_t st) {
+cudaError_t launch_token_plan(const int32_t* idx, int F, int k, int N, int32_t* hist, int32_t* offsets,
+                              int32_t* perm, int32_t* inv, int32_t* status, cudaStream_t st) {
   if (F <= kPlanThreads * kPlanBlocks) return run_plan<1>(idx, F, k, N, offsets, perm, inv, status, st);
-  return run_plan<kPlanMost>(idx, F, k, N, offsets, perm, inv, status, st);
+  if (F <= kPlanThreads * kPlanBlocks * 2) return run_plan<2>(idx, F, k, N, offsets, perm, inv, status, st);
+  if (F <= kPlanThreads * kPlanBlocks * 4) return run_plan<4>(idx, F, k, N, offsets, perm, inv, status, st);
+  const dim3 grid((F + kLargeSlots - 1) / kLargeSlots);
+  auto smem = [](int experts) { return sizeof(int) * static_cast<size_t>(experts) * (32 * kLargeMost + 2); };
+  cudaError_t err = cudaFuncSetAttribute(plan_place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(smem(kMaxExperts)));
+  if (err == cudaSuccess)
+    err = launch_pdl(plan_count_kernel, grid, dim3(kPlanThreads), 0, st, 1, idx, F, k, N, hist, status);
+  if (err != cudaSuccess) return err;
+  return launch_pdl(plan_place_kernel, grid, dim3(kPlanThreads), smem(N), st, 1, idx, F, k, N,
+                    static_cast<const int32_t*>(hist), offsets, perm, inv);
 }
 
 cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st) {

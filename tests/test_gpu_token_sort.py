@@ -16,7 +16,7 @@ DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 EPS = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}  # half a unit in the last place
 SHAPES = [  # T, d, N, k
     (1, 1, 1, 1), (1, 7168, 256, 8), (2, 9, 3, 2), (5, 64, 8, 8), (33, 130, 60, 4), (128, 1024, 128, 8),
-    (129, 1023, 6, 6), (300, 257, 40, 32), (700, 2048, 128, 8), (1500, 40, 256, 3), (40, 8200, 16, 2), (1500, 9, 250, 8), (4000, 16, 256, 8), (4097, 8, 64, 8), (9000, 4, 7, 3),
+    (129, 1023, 6, 6), (300, 257, 40, 32), (700, 2048, 128, 8), (1500, 40, 256, 3), (40, 8200, 16, 2), (1500, 9, 250, 8), (4000, 16, 256, 8), (4097, 8, 64, 8), (9000, 4, 7, 3), (7000, 4, 40, 3), (4097, 3, 250, 5),
     (17, 1028, 16, 5), (9, 20001, 16, 5)]
 
 
@@ -166,6 +166,24 @@ def test_agrees_with_the_layer_forward():
     B.check(B.pr2_moe_forward(dm, h, idx, gates, *W, None, None, None, out, counts, perm, B.alloc_workspace(dm)))
     offsets, perm2, inv, _ = sort(dm, idx, None, None)
     assert torch.equal(perm, perm2) and torch.equal(counts, offsets.diff())
+
+
+@pytest.mark.parametrize("T,N,k", [(200000, 128, 8), (600000, 60, 8), (1100000, 5, 4)])
+def test_plans_of_many_slots(T, N, k):
+    """Sizes where the plan is made by blocks, and (over 4 M slots) by the layer's dispatch."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    idx = torch.rand(T, N, generator=g, device="cuda").topk(k, 1).indices.int().contiguous()
+    idx[torch.rand(T, generator=g, device="cuda") < 0.1] = -1
+    flat = idx.reshape(-1).long()
+    ranked, order = torch.sort(torch.where(flat >= 0, flat, N), stable=True)
+    offsets, perm, inv, status = sort(B.dims(T, 8, N, k, 1, 0, "bf16"), idx, None, None)
+    want = torch.searchsorted(ranked, torch.arange(N + 1, device="cuda"))
+    assert torch.equal(offsets.long(), want) and status == B.PR2_STATUS_BAD_INDEX
+    used = int(want[N])
+    assert torch.equal(perm[:used].long(), order[:used]) and (perm[used:] == -1).all()
+    place = torch.full_like(flat, -1)
+    place[order[:used]] = torch.arange(used, device="cuda")
+    assert torch.equal(inv.long(), place)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
