@@ -333,7 +333,7 @@ typedef struct {
  *     c_t = w_t (kl_coef (1 - exp gap) - (shut ? 0 : r A)).
  *  logits [T, ld_logits] dtype; target [T] int32; weight [T] fp32 (NULL: 1/T): mask and
  *    normalisation in one.  A token of weight 0 contributes nothing, whatever its other inputs
- *    hold (they are not read): logp, entropy and its gradient row are 0.
+ *    hold (its logits are not read): logp, entropy and its gradient row are 0.
  *  advantage [T] fp32; logp_old [T] fp32 (NULL: logp itself, r = 1, an on-policy step);
  *    logp_ref [T] fp32 (NULL only if kl_coef is 0; K is then 0, also in loss[2]).
  *  loss [4] fp32 out (summed in double in a fixed order); logp [T], entropy [T] fp32 out, nullable;

@@ -764,16 +764,17 @@ cudaError_t sum_rows(const TokenArgs& a, int num_sms, cudaStream_t st) {
                     static_cast<T*>(a.dst));
 }
 
-// unsort_backward: a block a token for few tokens, and for rows of a piece or more a warp while a warp a
-// token would leave the SMs unevenly filled; else a warp a token (bf16, k = 8, us with a warp / a block:
-// 4096 x 2048 60.2 / 47.3, 8192 x 7168 341 / 321, 32768 x 2048 351 / 374, 4096 x 512 14.0 / 26.1).
+// unsort_backward: a block a token for few tokens, and for tokens of much work (eight pieces of a row for
+// each warp) while a warp a token would leave the SMs unevenly filled; else a warp a token (bf16, k = 8, us
+// with a warp / a block: 4096 x 2048 60.2 / 47.3, 8192 x 7168 341 / 321, 32768 x 2048 351 / 374, 4096 x 512
+// 14.0 / 26.1).
 template <typename T>
 cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
                                                  int, int, int, T*, float*),
                                    void (*blocks)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
                                                   int, int, int, T*, float*),
                                    int pieces, const TokenArgs& a, int num_sms, cudaStream_t st) {
-  const bool many = a.T >= static_cast<int64_t>(num_sms) * (pieces >= kWarps ? 64 : 2);
+  const bool many = a.T >= static_cast<int64_t>(num_sms) * (pieces * a.k >= kWarps * 8 ? 64 : 2);
   return launch_pdl(many ? warps : blocks, dim3(blocks_for(a.T, many ? kWarps : 1, num_sms, 16)), dim3(kThreads), 0, st,
                     1, static_cast<const T*>(a.src), static_cast<const T*>(a.y), a.gates, a.inv, a.offsets,
                     static_cast<int>(a.T), a.d, a.N, a.k, static_cast<T*>(a.dst), a.dgates);
