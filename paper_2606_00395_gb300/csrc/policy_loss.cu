@@ -35,7 +35,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // ---- packed pairs of fp32 -------------------------------------------------------------------
@@ -425,15 +424,35 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
     }
     return g;
   }
-  const float logl = logf(s.l);
+  const float mean = s.e / s.l;
   const float M = scaled_ref(s.m, scale);
-  const float logp = fmaf(power_of(in.za, s.m, M, scale), kLn2, -logl);
+  // The target's y, and in `slip` what log 2 times it lacks: the rest of its product and differences,
+  // and to first order what rounding scale and log 2 to 32 bits did to every y (the same to all tokens,
+  // so that it would not average out in the loss): scale_slip moves a y by its own multiple, log l by
+  // that of the mean y.  l = 2^n part with 1 <= part < 2, so logp = (y - n) log 2 - log part, and its
+  // distance from another log-probability x is taken as one fused product less x: the ratio does not
+  // lose what the logarithm of a large l would.  (A NaN or infinity stays in part; an infinite y, a
+  // target that is banned, has no rest.)
+  const uint32_t bits = __float_as_uint(s.l);
+  const int n = bits < 0x7f800000u ? static_cast<int>(bits >> 23) - 127 : 0;
+  const float log_part = logf(__uint_as_float(bits - (static_cast<uint32_t>(n) << 23)));
+  const float p = in.za * scale, nf = static_cast<float>(n);
+  const float y = M == M ? p - M : (in.za - s.m) * scale, yn = y - nf;
+  float slip = 0.f;
+  if (fabsf(y) < CUDART_INF_F) {
+    const float back = y - p, back_n = yn - y;
+    float rest = (y - (yn - back_n)) - (nf + back_n);
+    if (M == M) rest += fmaf(in.za, scale, -p) + ((p - (y - back)) - (M + back));
+    slip = fmaf(rest, kLn2, fmaf(y, a.log_slip, -a.scale_slip * mean));
+  }
+  auto logp_less = [&](float x) { return fmaf(yn, kLn2, -x) - log_part + slip; };
+  const float logp = logp_less(0.f);
   if (write) {
     if (a.logp != nullptr) a.logp[k.t] = logp;
-    if (a.entropy != nullptr) a.entropy[k.t] = fmaf(-kLn2, s.e / s.l, logl);
+    if (a.entropy != nullptr) a.entropy[k.t] = fmaf(kLn2, nf - mean, log_part);
   }
   const float A = in.A;
-  const float r = a.logp_old != nullptr ? expf(logp - in.old) : 1.f;
+  const float r = a.logp_old != nullptr ? expf(logp_less(in.old)) : 1.f;
   const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
   // min(r A, clip(r) A) takes the clipped side exactly where the clip shuts the gradient off; a NaN
   // ratio goes through.  A token of advantage 0 has no policy part, however large its ratio.
@@ -442,7 +461,7 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   float c = shut || A == 0.f ? 0.f : -r * A;
   float kl = 0.f;
   if (a.logp_ref != nullptr) {
-    const float gap = in.ref - logp, x = expm1f(gap);
+    const float gap = -logp_less(in.ref), x = expm1f(gap);
     kl = isinf(x) ? x : x - gap;
     if (a.kl_coef > 0.f) c -= a.kl_coef * x;
   }
@@ -641,7 +660,7 @@ __global__ void __launch_bounds__(kRowThreads, 3)
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.status)) != 0;
     };
-    const float scale = a.inv_temp * kLog2e;
+    const float scale = a.scale;
     T* grad = static_cast<T*>(a.grad);
     RingAt in_at{0, 0u}, out_at{0, 0u};  // the next chunk to come, the next one to let go
     double sums[3] = {0.0, 0.0, 0.0};
@@ -771,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kern
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const float scale = a.inv_temp * kLog2e;
+  const float scale = a.scale;
   double sums[3] = {0.0, 0.0, 0.0};
   const int rows = static_cast<int>(gridDim.x) * kWarps;
   for (int t = static_cast<int>(blockIdx.x) * kWarps + warp; t < a.T; t += rows) {
@@ -906,7 +925,13 @@ int active_clusters(int C) {
 }
 
 template <typename T>
-cudaError_t launch(const PolicyArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
+  PolicyArgs a = args;
+  const double exact = static_cast<double>(a.inv_temp) * 1.4426950408889634, log2 = 0.6931471805599453;
+  a.scale = static_cast<float>(exact);
+  const double slip = exact / a.scale - 1.0;
+  a.scale_slip = static_cast<float>(log2 * slip);
+  a.log_slip = static_cast<float>(log2 * (1.0 + slip) - static_cast<double>(kLn2));
   constexpr int E = Vec<T>::kElems;
   const int64_t nvec = a.V / E;  // most whole vectors of a row
   const int64_t resident = static_cast<int64_t>(num_sms) * kCtasPerSm;

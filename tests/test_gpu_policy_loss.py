@@ -155,6 +155,37 @@ def test_banned_entries_and_empty_rows(dtype):
     assert not got["grad"][c["logits"] == -math.inf].any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [300, 9000])
+def test_a_target_that_is_banned(V, dtype):
+    """Its probability is 0: logp -inf, ratio 0, no gradient (without a KL term)."""
+    c = make(5, V, dtype, 17)
+    c["weight"][:] = 0.2
+    c["advantage"][:] = torch.tensor([1.0, 1.0, -1.0, 0.0, 2.0])
+    for t in (1, 2, 3):
+        c["logits"][t, c["target"][t].long()] = -math.inf
+    got = call(c, dtype, names=("weight", "logp_old"))
+    assert (got["logp"][1:4] == -math.inf).all() and torch.isfinite(got["entropy"]).all()
+    assert not got["grad"][1:4].any() and torch.isfinite(got["loss"]).all() and torch.isfinite(got["grad"]).all()
+    check(c, got, dtype, names=("weight", "logp_old"))
+    onp = call(c, dtype, names=("weight",))  # on-policy: the ratio is 1 by definition
+    assert (onp["logp"][1:4] == -math.inf).all() and torch.isfinite(onp["loss"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("offset", [-3000.0, -70.0, 45.0, 500.0])
+def test_logits_with_an_offset(offset, dtype):
+    """The sums' reference is 0 to begin with; rows far from it are summed relative to their maximum.  The
+    offset is exact in either type only where the logits are on its grid."""
+    c = make(6, 5000, dtype, 18, std=1.0)
+    c["logits"][:, :5000] = (c["logits"][:, :5000].float() * 0.25).round() * 16 + offset
+    base = torch.log_softmax(c["logits"][:, :5000].double(), 1)[torch.arange(6), c["target"].long()]
+    c["weight"][:] = 0.15
+    c["logp_old"], c["logp_ref"] = (base - 0.05).float(), (base + 0.1).float()
+    kw = dict(kl_coef=0.05)
+    check(c, call(c, dtype, **kw), dtype, **kw)
+
+
 def test_tokens_that_do_not_count_are_not_read():
     c = make(20, 500, "bf16", 9)
     kw = dict(kl_coef=0.05)
