@@ -6,6 +6,8 @@
  *             pr2_old_output; Algorithm 1 rollout steps, Algorithm 2)
  *   training: pr2_route_replay   then  pr2_moe_forward   (Sec. 4.1 "Replay During Training",
  *             Eq. pr2_output; Algorithm 1 replay steps, Algorithm 3)
+ * Further on: the predictive loss, diagnostics, the multi-layer loop, and ("training side") the
+ * policy loss and the gradient operators of the layer.
  *
  * Conventions shared by every entry point:
  *  - Every tensor argument is a DEVICE pointer to a contiguous row-major buffer owned by the

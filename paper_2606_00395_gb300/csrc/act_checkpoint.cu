@@ -6,6 +6,8 @@
 // Bound by HBM: bf16 reads 4 bytes and writes 4 per element forward, reads 4 and writes 6 backward.
 // Lanes take 8 neighbouring elements (two 16-byte vectors of fp32, one of bf16; 8 bytes of q), so 16
 // lanes hold a run and a warp two; where a row's start or width does not allow that, single elements.
+// 32768 x 768 bf16: forward 38 us (79 % of the copy rate; it issues about 30 instructions an element, 79 %
+// of all slots), backward 41 us (91 %); 65536 x 2048 88 % and 95 %; 767 columns 64 and 68 us.
 #include "pr2_device.cuh"
 #include "pr2_internal.h"
 

@@ -13,7 +13,9 @@
 // All of it is bound by HBM: the k expert rows, read or written once.  A warp takes a piece of a
 // token's row, a lane V neighbouring columns: 16 bytes where d and the pointers allow it, else one
 // fp32 element or a pair of bf16 ones (a row of odd width starts at any element, so a row's pairs
-// start at its first column or at its second, whichever lies on 4 bytes).
+// start at its first column or at its second, whichever lies on 4 bytes).  bf16, k = 8, back to back:
+// 32768 x 2048 sorted in 190 us (94 % of the copy rate), summed in 185 (96 %), unsort gradient 351 (96 %);
+// 4096 x 2047 (pairs) 28, 57 and 82 us against 21, 23 and 48 for 2048 columns.
 #include "pr2_device.cuh"
 #include "pr2_internal.h"
 

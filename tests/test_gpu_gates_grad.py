@@ -35,7 +35,8 @@ def call(probs, idx, dg, norm):
 
 @pytest.mark.parametrize("norm", [False, True])
 @pytest.mark.parametrize("T,N,k", [(1, 1, 1), (1, 8, 8), (7, 5, 3), (33, 60, 4), (130, 128, 8), (65, 256, 32),
-                                   (9, 33, 32), (300, 129, 1), (12, 250, 7)])
+                                   (9, 33, 32), (300, 129, 1), (12, 250, 7),
+                                   (77, 32, 8), (50, 24, 9), (61, 64, 16), (40, 64, 17), (1000, 60, 8), (3, 4, 4), (2000, 256, 8)])
 def test_matches_the_formula(T, N, k, norm):
     probs, idx, dg = case(T, N, k, T + N + k)
     got, status = call(probs, idx, dg, norm)
