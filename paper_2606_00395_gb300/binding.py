@@ -103,6 +103,8 @@ def library_path() -> str:
 def load() -> ctypes.CDLL:
     """Load ``libpr2.so`` (built by ``paper_2606_00395_gb300.build``); raise if it is absent."""
     global _lib
+    if _lib is not None:  # (set once, after its signatures)
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
