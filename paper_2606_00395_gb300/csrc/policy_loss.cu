@@ -1,9 +1,8 @@
 // Clipped policy loss with a KL term over a vocabulary, and the gradient of the logits
 // (pr2_policy_loss).
 //
-// A row needs its maximum m, l = sum exp(z - m) and, for the entropy H = log l - e / l,
-// e = sum exp(z - m) (z - m): one pass keeps a running maximum with the two sums, rescaled when it
-// grows.  The token's loss and the factor of its gradient,
+// A row needs, relative to any m, l = sum exp(z - m) and, for the entropy H = log l - e / l,
+// e = sum exp(z - m) (z - m): one pass.  The token's loss and the factor of its gradient,
 //   c = w (beta (1 - exp(gap)) - (shut ? 0 : r A)),
 // depend on the target's log-probability alone, so a second pass over the row writes
 //   grad_v = f [v = a] - (f / l) exp(z_v - m),  f = grad_scale inv_temp c
@@ -20,8 +19,9 @@
 // the order of loading and of release the ring is first in, first out throughout.  The slots that the
 // second pass frees take the next row's chunks.  The CTAs of a cluster may split a row: they exchange
 // their three sums through distributed shared memory.  Short rows go to one warp each.
-// Bound by HBM (logits read once, gradient written once), and per row by its serial part, about 3 us of
-// joins, exchange and the token's own arithmetic, which three CTAs an SM overlap.  Back to back, without
+// Bound by HBM (logits read once, gradient written once), and per row by its serial part, some 3 us of
+// joins, exchange and the token's own arithmetic, which the CTAs of an SM overlap; rows of a few KB by what
+// each warp issues per row, so they have CTAs of fewer warps.  Back to back, without
 // masked tokens: 4096 x 131072 bf16 396 us with the gradient (80 % of the copy rate), 161 without (98 %);
 // 8192 x 32001 178 us (87 %); 2048 x 131072 fp32 384 us (82 %); 32768 x 2048 (warps) 72 us (55 %, the
 // token's arithmetic); one token of 131072 7.3 us.
@@ -489,10 +489,15 @@ __device__ __forceinline__ void write_loss(const PolicyArgs& a, const double (&s
 }
 
 // ---- rows through a ring of chunks -----------------------------------------------------------------
-constexpr int kRing = 4;             // chunks of a CTA's ring
-constexpr int kChunkVecs = 1024;     // 16-byte vectors of a chunk
-constexpr int kChunkBytes = kChunkVecs * 16;
-constexpr int kRowThreads = kThreads + 32;  // eight consumer warps, one producer
+// Consumer warps of a CTA, its ring, and CTAs an SM.  Bf16 rows, T = 4096, us with wide / narrow: V = 5128
+// 40.0 / 31.1, 8192 40.8 / 36.0, 12000 52.5 / 45.4, 24000 74.8 / 77.5, 50001 155 / 169.
+struct WideRows {
+  static constexpr int kWarps = 8, kRing = 4, kChunkVecs = 1024, kCtas = 3;
+};
+struct NarrowRows {
+  static constexpr int kWarps = 4, kRing = 5, kChunkVecs = 512, kCtas = 5;
+};
+constexpr int kNarrowVecs = 1536;  // most vectors of a row for NarrowRows
 constexpr int kTokens = 2;  // token records ahead of the consumers
 
 // A row's token as the producer hands it to the consumers.
@@ -503,6 +508,7 @@ struct TokenRecord {
 };
 
 // A place in the ring: slot and how often the ring went round (its parity).
+template <int kRing>
 struct RingAt {
   int slot;
   uint32_t round;
@@ -555,9 +561,11 @@ struct Slice {
 };
 
 // C CTAs a row, `cap` vectors each at most.
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads, 3)
+template <typename T, typename Rows>
+__global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
     policy_row_kernel(const PolicyArgs a, int C, int cap) {
+  constexpr int kWarps = Rows::kWarps, kThreads = 32 * kWarps, kRing = Rows::kRing;
+  constexpr int kChunkVecs = Rows::kChunkVecs;
   extern __shared__ uint4 ring[];
   __shared__ float4 part[2][kWarps];
   __shared__ float4 xchg[2][kMaxCluster];
@@ -610,7 +618,7 @@ __global__ void __launch_bounds__(kRowThreads, 3)
   if (warp == kWarps) {
     // ---------------- producer ----------------
     if (lane == 0) {
-      RingAt at{0, 0u};
+      RingAt<kRing> at{0, 0u};
       uint32_t landing = 0, last_round = 0;  // slots with a copy issued, and its round
       // a token's row number, weight and inputs are loaded two rows ahead, its target's logit one ahead
       Token cur = load_token(a, first), next = load_token(a, first + groups);
@@ -667,7 +675,7 @@ __global__ void __launch_bounds__(kRowThreads, 3)
     };
     const float scale = a.scale;
     T* grad = static_cast<T*>(a.grad);
-    RingAt in_at{0, 0u}, out_at{0, 0u};  // the next chunk to come, the next one to let go
+    RingAt<kRing> in_at{0, 0u}, out_at{0, 0u};  // the next chunk to come, the next one to let go
     double sums[3] = {0.0, 0.0, 0.0};
     uint32_t live = 0;  // rows joined so far
     auto let_go = [&] {
@@ -884,18 +892,17 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(const PolicyArgs a, 
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-constexpr size_t kRingBytes = static_cast<size_t>(kRing) * kChunkBytes;
-constexpr int kCtasPerSm = 3;
-static_assert(kCtasPerSm * (kRingBytes + 2048) <= 227 * 1024, "three rings an SM");
-
-template <typename T>
-cudaError_t set_smem() {
-  return cudaFuncSetAttribute(policy_row_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(kRingBytes));
+template <typename Rows>
+constexpr size_t ring_bytes() {
+  return static_cast<size_t>(Rows::kRing) * Rows::kChunkVecs * 16;
 }
+static_assert(WideRows::kCtas * (ring_bytes<WideRows>() + 2048) <= 227 * 1024 &&
+                  NarrowRows::kCtas * (ring_bytes<NarrowRows>() + 2048) <= 227 * 1024,
+              "the CTAs' rings fit an SM");
+static_assert(kNarrowVecs <= NarrowRows::kRing * NarrowRows::kChunkVecs, "a narrow row fits its ring");
 
 // Clusters of C CTAs of the row kernel that run at once (0 on error), cached per device and C.
-template <typename T>
+template <typename T, typename Rows>
 int active_clusters(int C) {
   struct Entry {
     int dev, C, clusters;
@@ -910,8 +917,8 @@ int active_clusters(int C) {
     if (cache[i].dev == dev && cache[i].C == C) return cache[i].clusters;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(C);
-  cfg.blockDim = dim3(kRowThreads);
-  cfg.dynamicSmemBytes = kRingBytes;
+  cfg.blockDim = dim3(32 * (Rows::kWarps + 1));
+  cfg.dynamicSmemBytes = ring_bytes<Rows>();
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = C;
@@ -920,13 +927,28 @@ int active_clusters(int C) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int n = 0;
-  if (set_smem<T>() != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, policy_row_kernel<T>, &cfg) != cudaSuccess) {
+  auto* kernel = policy_row_kernel<T, Rows>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(ring_bytes<Rows>())) !=
+          cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
     (void)cudaGetLastError();
     return 0;
   }
   if (used < 32) cache[used++] = Entry{dev, C, n};
   return n;
+}
+
+// Rows over clusters of C CTAs; *parts: the clusters that take rows.
+template <typename T, typename Rows>
+cudaError_t launch_rows(const PolicyArgs& a, int64_t nvec, int C, int64_t* parts, cudaStream_t st) {
+  int64_t groups = active_clusters<T, Rows>(C);
+  if (groups <= 0) return cudaErrorInvalidConfiguration;
+  if (groups > a.T) groups = a.T;
+  if (groups > kPolicyParts) groups = kPolicyParts;
+  *parts = groups;
+  return launch_pdl(policy_row_kernel<T, Rows>, dim3(static_cast<unsigned>(groups * C)),
+                    dim3(32 * (Rows::kWarps + 1)), ring_bytes<Rows>(), st, C, a, C,
+                    static_cast<int>((nvec + C - 1) / C));
 }
 
 template <typename T>
@@ -939,8 +961,8 @@ cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
   a.log_slip = static_cast<float>(log2 * (1.0 + slip) - static_cast<double>(kLn2));
   constexpr int E = Vec<T>::kElems;
   const int64_t nvec = a.V / E;  // most whole vectors of a row
-  const int64_t resident = static_cast<int64_t>(num_sms) * kCtasPerSm;
-  int64_t parts;
+  const int64_t resident = static_cast<int64_t>(num_sms) * WideRows::kCtas;
+  int64_t parts = 0;
   cudaError_t err;
   // A warp a row up to 4 KB, and up to 8 KB where the rows outnumber the CTAs that the row kernel keeps
   // resident (bf16 rows of 4096, us: 256 rows 11.3 by warps, 8.8 by rows; 2432 rows 13.3 / 24.6; rows
@@ -953,6 +975,8 @@ cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
     err = nvec <= 128 ? launch_pdl(policy_warp_kernel<T, 4>, grid, dim3(kThreads), 0, st, 1, a)
           : nvec <= 256 ? launch_pdl(policy_warp_kernel<T, 8>, grid, dim3(kThreads), 0, st, 1, a)
                       : launch_pdl(policy_warp_kernel<T, 16>, grid, dim3(kThreads), 0, st, 1, a);
+  } else if (nvec <= kNarrowVecs && a.T > resident) {
+    err = launch_rows<T, NarrowRows>(a, nvec, 1, &parts, st);
   } else {
     // CTAs a row.  A row that does not fit the rings is read again from L2, so the rows in flight have to
     // stay there (with the gradients on their way, 48 of its 129 MB): 4096 bf16 rows of 65536 take 220 us
@@ -961,17 +985,11 @@ cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
     // cluster too while that puts idle CTAs to work and leaves every thread four vectors.
     int C = 1;
     if (a.grad != nullptr)
-      while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * kRingBytes) &&
+      while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * ring_bytes<WideRows>()) &&
              (a.T < resident / C ? a.T : resident / C) * nvec * 16 > (int64_t{48} << 20))
         C *= 2;
     while (C < kMaxCluster && a.T * C * 2 <= resident && nvec >= C * 4 * kThreads) C *= 2;
-    int64_t groups = active_clusters<T>(C);
-    if (groups <= 0) return cudaErrorInvalidConfiguration;
-    if (groups > a.T) groups = a.T;
-    if (groups > kPolicyParts) groups = kPolicyParts;
-    parts = groups;
-    err = launch_pdl(policy_row_kernel<T>, dim3(static_cast<unsigned>(groups * C)), dim3(kRowThreads),
-                     kRingBytes, st, C, a, C, static_cast<int>((nvec + C - 1) / C));
+    err = launch_rows<T, WideRows>(a, nvec, C, &parts, st);
   }
   if (err != cudaSuccess || parts == 1) return err;  // one cluster (block) writes the loss itself
   return launch_pdl(policy_finish_kernel, dim3(1), dim3(256), 0, st, 1, a, static_cast<int>(parts));

@@ -84,7 +84,7 @@ def check(c, got, dtype, names=("weight", "logp_old", "logp_ref"), **kw):
 @pytest.mark.parametrize("T,V,pad,shift", [
     (1, 1, 0, 0), (1, 2, 0, 1), (3, 7, 1, 0), (5, 33, 0, 3), (4, 255, 0, 1), (7, 1000, 24, 0),
     (2, 4097, 0, 5), (9, 8192, 0, 0), (300, 515, 0, 0), (700, 64, 0, 0), (3, 32001, 0, 0),
-    (1, 70003, 0, 0), (2, 131072, 8, 8), (1, 300001, 0, 1)])
+    (1, 70003, 0, 0), (2, 131072, 8, 8), (1, 300001, 0, 1), (1000, 5003, 0, 1), (600, 6000, 1, 0)])
 def test_loss_and_gradient(dtype, T, V, pad, shift):
     c = make(T, V, dtype, T * 31 + V, pad=pad, shift=shift)
     kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05)
