@@ -632,16 +632,16 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
         const TokenIn after_in = load_inputs(a, next.t + groups);
         check_token(a, next, rank == 0);
         next_in.za = load_target<T>(a, next);
-        const int rec = row % kTokens;
-        ok = mbar_wait(&read[rec], ((row / kTokens) & 1u) ^ 1u, abort_flag, a.status);
-        if (!ok) break;
-        record[rec] = TokenRecord{cur.w, cur.target, cur_in};
-        mbar_arrive(&told[rec]);
+        Slice s{};
+        const char* src = nullptr;
+        int again = 0;
         if (cur.w != 0.f) {
-          const Slice s = slice_of(cur.t);
-          const char* src = reinterpret_cast<const char*>(row_of(cur.t) + s.sh.head) + static_cast<int64_t>(v0) * 16;
-          const int again = hold && s.chunks > kRing ? s.chunks - kRing : 0;
-          for (int i = 0; i < s.chunks + again && ok; ++i) {
+          s = slice_of(cur.t);
+          src = reinterpret_cast<const char*>(row_of(cur.t) + s.sh.head) + static_cast<int64_t>(v0) * 16;
+          again = hold && s.chunks > kRing ? s.chunks - kRing : 0;
+        }
+        auto load_chunks = [&](int from, int to) {
+          for (int i = from; i < to && ok; ++i) {
             const int v = (i < s.chunks ? i : i - s.chunks) * kChunkVecs;
             const int left = s.n - v;
             const uint32_t bytes = static_cast<uint32_t>(left < kChunkVecs ? left : kChunkVecs) * 16u;
@@ -653,7 +653,17 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
             last_round = (last_round & ~(1u << at.slot)) | (at.round << at.slot);
             at.step();
           }
-        }
+        };
+        // The first row's chunks go on their way before the record is told, which waits for the target's
+        // logit; later on the consumers may need the record to free a chunk.
+        const int chunks = s.chunks + again, early = row > 0 ? 0 : chunks < kRing ? chunks : kRing;
+        load_chunks(0, early);
+        const int rec = row % kTokens;
+        if (ok) ok = mbar_wait(&read[rec], ((row / kTokens) & 1u) ^ 1u, abort_flag, a.status);
+        if (!ok) break;
+        record[rec] = TokenRecord{cur.w, cur.target, cur_in};
+        mbar_arrive(&told[rec]);
+        load_chunks(early, chunks);
         cur = next;
         cur_in = next_in;
         next = after;
@@ -876,14 +886,18 @@ __global__ void __launch_bounds__(256) policy_finish_kernel(const PolicyArgs a, 
   __shared__ double sh[3][256];
   pdl_wait();
   pdl_trigger();
+  // (64-bit additions are slow here: none of zeros)
+  const int tid = threadIdx.x;
   double s[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < n; i += 256)
+  if (tid < n)
+    for (int j = 0; j < 3; ++j) s[j] = a.partial[tid * 4 + j];
+  for (int i = tid + 256; i < n; i += 256)
     for (int j = 0; j < 3; ++j) s[j] += a.partial[i * 4 + j];
-  for (int j = 0; j < 3; ++j) sh[j][threadIdx.x] = s[j];
+  for (int j = 0; j < 3; ++j) sh[j][tid] = s[j];
   for (int o = 128; o > 0; o >>= 1) {
     __syncthreads();
-    if (threadIdx.x < o)
-      for (int j = 0; j < 3; ++j) sh[j][threadIdx.x] += sh[j][threadIdx.x + o];
+    if (tid < o && tid + o < n)
+      for (int j = 0; j < 3; ++j) sh[j][tid] += sh[j][tid + o];
   }
   if (threadIdx.x == 0) {
     const double all[3] = {sh[0][0], sh[1][0], sh[2][0]};
