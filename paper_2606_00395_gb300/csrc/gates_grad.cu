@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(kWarps * 32)
 cudaError_t launch_gates_backward(const float* probs, const int32_t* idx, const float* dgates,
                                   int64_t T, int N, int k, bool norm, float* dlogits,
                                   int32_t* status, int num_sms, cudaStream_t st) {
-  const bool vec = N % 4 == 0 && ((reinterpret_cast<uintptr_t>(probs) | reinterpret_cast<uintptr_t>(dlogits)) & 15u) == 0;
+  const bool vec =
+      N % 4 == 0 && ((reinterpret_cast<uintptr_t>(probs) | reinterpret_cast<uintptr_t>(dlogits)) & 15u) == 0;
   const int lanes = !vec || N > 64 || k > 16 ? 32 : N > 32 || k > 8 ? 16 : 8;
   const int per_block = kWarps * 32 / lanes;
   int64_t blocks = (T + per_block - 1) / per_block;

@@ -779,7 +779,8 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
           }
           if (!ok) break;
         } else {
-          grad_span<T, kThreads, kChunkVecs>([](int) { return make_uint4(0u, 0u, 0u, 0u); }, out, sl.n, tid, g, scale, -1);
+          grad_span<T, kThreads, kChunkVecs>([](int) { return make_uint4(0u, 0u, 0u, 0u); }, out, sl.n, tid, g, scale,
+                                             -1);
         }
         if (edge >= 0)
           grad[cur.t * a.ld_grad + edge] =
@@ -857,7 +858,8 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kern
       for (int j = 0; j < kHeld; ++j) {
         const int left = sh.nvec - j * 32, e0 = sh.head + j * 32 * Vec<T>::kElems;
         if (left > 0)
-          grad_span<T, 32, 32>([&](int) { return raw[j]; }, out + e0, left < 32 ? left : 32, lane, g, scale, k.target - e0);
+          grad_span<T, 32, 32>([&](int) { return raw[j]; }, out + e0, left < 32 ? left : 32, lane, g, scale,
+                               k.target - e0);
       }
       if (edge >= 0)
         out[edge] = g.f != 0.f ? grad_one<T>(ez, g, scale, edge == k.target) : from_f32<T>(0.f);

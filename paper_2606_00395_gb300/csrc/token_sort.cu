@@ -120,7 +120,9 @@ __device__ __forceinline__ void fill_perm(int32_t* __restrict__ perm, int from, 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanBlocks = 8;
 
-constexpr size_t plan_smem_bytes(int N, int S) { return sizeof(int) * static_cast<size_t>(N) * (32 * S + kPlanBlocks + 1); }
+constexpr size_t plan_smem_bytes(int N, int S) {
+  return sizeof(int) * static_cast<size_t>(N) * (32 * S + kPlanBlocks + 1);
+}
 
 // The lanes with the same e (-1 <= e < N) as this one: a ballot per bit, which takes less than a
 // __match_any_sync (placing 4096 slots of a block 1 us less, counting them so 3 us).
@@ -498,7 +500,8 @@ __global__ void __launch_bounds__(kThreads)
   constexpr int kTokens = kWarps / G;  // of a block at once
   const int g_warp = warp % G;
   // (whole blocks go round together: with G > 1 they meet at a barrier)
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < Tn; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kTokens;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < Tn; t0 += step) {
     const int64_t t = t0 + warp / G;
     if (G == 1 && t >= Tn) break;
     for (int s0 = 0; s0 < k; s0 += kSlots) {
@@ -691,7 +694,8 @@ __global__ void __launch_bounds__(kThreads)
   pdl_trigger();
   const int F = Tn * k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = pairs_of(d);
   constexpr int kTokens = kWarps / G;
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < Tn; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kTokens;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < Tn; t0 += step) {
     const int64_t t = t0 + warp / G;
     if (G == 1 && t >= Tn) break;
     for (int s0 = 0; s0 < k; s0 += kSlots) {
@@ -712,7 +716,8 @@ __global__ void __launch_bounds__(kThreads)
             const int r = __shfl_sync(0xffffffffu, mine, s);
             const bf16* row = y + static_cast<int64_t>(r) * d;
 #pragma unroll
-            for (int u = 0; u < U; ++u) raw[s][u] = r >= 0 ? load_pair(row, 2 * (j0 + u * 32) - row_parity(row), d) : 0u;
+            for (int u = 0; u < U; ++u)
+              raw[s][u] = r >= 0 ? load_pair(row, 2 * (j0 + u * 32) - row_parity(row), d) : 0u;
           }
 #pragma unroll
           for (int s = 0; s < kSlots; ++s) {
@@ -806,8 +811,8 @@ cudaError_t launch_token_sort(const TokenArgs& a, int num_sms, cudaStream_t st) 
   constexpr int U = 4;
   const dim3 grid = a.dst != nullptr ? item_grid(a.T, pairs_of(a.d), U, num_sms)
                                      : dim3(blocks_for(a.T * a.k, kThreads, num_sms, 16));
-  return launch_pdl(sort_pairs_kernel<U>, grid, dim3(kThreads), 0, st, 1, static_cast<const bf16*>(a.src), a.inv, a.offsets, static_cast<int>(a.T), a.d, a.N, a.k,
-                    static_cast<bf16*>(a.dst), a.perm, a.status);
+  return launch_pdl(sort_pairs_kernel<U>, grid, dim3(kThreads), 0, st, 1, static_cast<const bf16*>(a.src), a.inv,
+                    a.offsets, static_cast<int>(a.T), a.d, a.N, a.k, static_cast<bf16*>(a.dst), a.perm, a.status);
 }
 cudaError_t launch_token_sum(const TokenArgs& a, int num_sms, cudaStream_t st) {
   if (!a.bf16) return vectors(a, 4) ? sum_rows<float, 4, 1>(a, num_sms, st) : sum_rows<float, 1, 2>(a, num_sms, st);
@@ -832,7 +837,8 @@ cudaError_t launch_token_unsort_backward(const TokenArgs& a, int num_sms, cudaSt
                                                       unsort_backward_kernel<bf16, 8, 1, kWarps>, a.d / 256, a,
                                                       num_sms, st)
                        : launch_unsort_backward<bf16>(unsort_backward_pairs_kernel<2, 1>,
-                                                      unsort_backward_pairs_kernel<2, kWarps>, a.d / 128, a, num_sms, st);
+                                                      unsort_backward_pairs_kernel<2, kWarps>, a.d / 128, a, num_sms,
+                                                      st);
 }
 
 }  // namespace pr2
