@@ -22,8 +22,8 @@
 // Bound by HBM (logits read once, gradient written once), and per row by its serial part, some 3 us of
 // joins, exchange and the token's own arithmetic, which the CTAs of an SM overlap; rows of a few KB by what
 // each warp issues per row, so they have CTAs of fewer warps.  Back to back, without
-// masked tokens: 4096 x 131072 bf16 396 us with the gradient (80 % of the copy rate), 161 without (98 %);
-// 8192 x 32001 178 us (87 %); 2048 x 131072 fp32 384 us (82 %); 32768 x 2048 (warps) 72 us (55 %, the
+// masked tokens: 4096 x 131072 bf16 361 us with the gradient (88 % of the copy rate), 161 without (98 %);
+// 8192 x 32001 178 us (87 %); 2048 x 131072 fp32 349 us (91 %); 32768 x 2048 (warps) 72 us (55 %, the
 // token's arithmetic); one token of 131072 7.3 us.
 // Tokens are dealt to clusters (warps) by their number; each sums its tokens' terms in double and
 // policy_finish_kernel the clusters' in order, so the loss does not depend on timing.
@@ -497,7 +497,15 @@ struct WideRows {
 struct NarrowRows {
   static constexpr int kWarps = 4, kRing = 5, kChunkVecs = 512, kCtas = 5;
 };
+// With the gradient a CTA's loads pause while its row's sums are joined, and a round has that cost however
+// short the slices are: long rows in large batches take fewer CTAs an SM with longer slices.  Bf16, T = 4096,
+// us with wide / deep: V = 50000 152 / 146, 65000 208 / 179, 98000 296 / 311, 131072 396 / 360, 260000 815 / 731;
+// T = 450, V = 65536 26.5 / 29.9 (two rounds against one and a half).  Forward alone wide is faster, 161 / 174.
+struct DeepRows {
+  static constexpr int kWarps = 8, kRing = 7, kChunkVecs = 1024, kCtas = 2;
+};
 constexpr int kNarrowVecs = 1536;  // most vectors of a row for NarrowRows
+constexpr int kDeepVecs = 6400;    // fewest vectors of a CTA's slice for DeepRows
 constexpr int kTokens = 2;  // token records ahead of the consumers
 
 // A row's token as the producer hands it to the consumers.
@@ -912,8 +920,10 @@ template <typename Rows>
 constexpr size_t ring_bytes() {
   return static_cast<size_t>(Rows::kRing) * Rows::kChunkVecs * 16;
 }
-static_assert(WideRows::kCtas * (ring_bytes<WideRows>() + 2048) <= 227 * 1024 &&
-                  NarrowRows::kCtas * (ring_bytes<NarrowRows>() + 2048) <= 227 * 1024,
+// (an SM has 228 KB, a CTA 1 KB of them for the system and less than 1 KB of its own beside the ring)
+static_assert(WideRows::kCtas * (ring_bytes<WideRows>() + 2048) <= 228 * 1024 &&
+                  NarrowRows::kCtas * (ring_bytes<NarrowRows>() + 2048) <= 228 * 1024 &&
+                  DeepRows::kCtas * (ring_bytes<DeepRows>() + 2048) <= 228 * 1024,
               "the CTAs' rings fit an SM");
 static_assert(kNarrowVecs <= NarrowRows::kRing * NarrowRows::kChunkVecs, "a narrow row fits its ring");
 
@@ -967,6 +977,21 @@ cudaError_t launch_rows(const PolicyArgs& a, int64_t nvec, int C, int64_t* parts
                     static_cast<int>((nvec + C - 1) / C));
 }
 
+// CTAs a row with the gradient.  A row that does not fit the rings is read again from L2, so the rows in
+// flight have to stay there (with the gradients on their way, `bytes` of its 129 MB: with WideRows 4096 bf16
+// rows of 65536 take 220 us with one CTA a row, 204 with two; with DeepRows 3400 rows of 175000 412 with two,
+// 472 with four, and of 103000 282 with one, 260 with two).  No more than that, because a round's exchange of
+// the sums takes its time however small the slices are (rows of 131072: 397 us with four, 510 with eight).
+template <typename Rows>
+int grad_cluster(int64_t T, int64_t nvec, int num_sms, int64_t bytes) {
+  int C = 1;
+  for (; C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * ring_bytes<Rows>()); C *= 2) {
+    const int64_t rows = static_cast<int64_t>(num_sms) * Rows::kCtas / C;
+    if ((T < rows ? T : rows) * nvec * 16 <= bytes) break;
+  }
+  return C;
+}
+
 template <typename T>
 cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
   PolicyArgs a = args;
@@ -994,18 +1019,16 @@ cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
   } else if (nvec <= kNarrowVecs && a.T > resident) {
     err = launch_rows<T, NarrowRows>(a, nvec, 1, &parts, st);
   } else {
-    // CTAs a row.  A row that does not fit the rings is read again from L2, so the rows in flight have to
-    // stay there (with the gradients on their way, 48 of its 129 MB): 4096 bf16 rows of 65536 take 220 us
-    // with one CTA a row, 204 with two.  No more than that, because a round's exchange of the sums takes
-    // its time however small the slices are (rows of 131072: 397 us with four, 510 with eight).  A wider
-    // cluster too while that puts idle CTAs to work and leaves every thread four vectors.
-    int C = 1;
-    if (a.grad != nullptr)
-      while (C < kMaxCluster && nvec * 16 > static_cast<int64_t>(C * ring_bytes<WideRows>()) &&
-             (a.T < resident / C ? a.T : resident / C) * nvec * 16 > (int64_t{48} << 20))
-        C *= 2;
-    while (C < kMaxCluster && a.T * C * 2 <= resident && nvec >= C * 4 * kThreads) C *= 2;
-    err = launch_rows<T, WideRows>(a, nvec, C, &parts, st);
+    // Wider clusters also where that puts idle CTAs to work and leaves every thread four vectors.
+    const int deep = a.grad == nullptr ? 1 : grad_cluster<DeepRows>(a.T, nvec, num_sms, int64_t{54} << 20);
+    if (a.grad != nullptr && nvec >= static_cast<int64_t>(deep) * kDeepVecs &&
+        a.T >= int64_t{4} * num_sms * DeepRows::kCtas) {
+      err = launch_rows<T, DeepRows>(a, nvec, deep, &parts, st);
+    } else {
+      int C = a.grad == nullptr ? 1 : grad_cluster<WideRows>(a.T, nvec, num_sms, int64_t{48} << 20);
+      while (C < kMaxCluster && a.T * C * 2 <= resident && nvec >= C * 4 * kThreads) C *= 2;
+      err = launch_rows<T, WideRows>(a, nvec, C, &parts, st);
+    }
   }
   if (err != cudaSuccess || parts == 1) return err;  // one cluster (block) writes the loss itself
   return launch_pdl(policy_finish_kernel, dim3(1), dim3(256), 0, st, 1, a, static_cast<int>(parts));

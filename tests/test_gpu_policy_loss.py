@@ -102,6 +102,40 @@ def test_many_rows_a_block(dtype):
     check(c, call(c, dtype, **kw), dtype, **kw)
 
 
+@pytest.mark.parametrize("dtype,T,V,pad,shift", [
+    ("bf16", 1217, 53001, 0, 1), ("bf16", 1300, 51200, 0, 0), ("bf16", 1300, 51199, 1, 0),
+    ("fp32", 1250, 27003, 5, 0), ("bf16", 1216, 107009, 0, 0), ("fp32", 1216, 66000, 0, 2),
+    ("bf16", 1240, 205001, 0, 0), ("bf16", 1215, 65536, 0, 0)])
+def test_long_rows_in_large_batches(dtype, T, V, pad, shift):
+    """61 different rows in turn, so that each meets the CTAs at several times and alignments."""
+    few = make(61, V, dtype, T + V)
+    which = torch.arange(T) % 61
+    c = {n: few[n][which] for n in ("target", "weight", "advantage", "logp_old", "logp_ref")}
+    ld = V + pad
+    buf = torch.full((T * ld + shift,), 1e4, dtype=DT[dtype])
+    logits = buf[shift:].view(T, ld)
+    logits[:, :V] = few["logits"][which]
+    c.update(buf=buf, shift=shift, ld=ld, V=V, logits=logits)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05)
+    got = call(c, dtype, **kw)
+    opt = {n: few[n] for n in ("logp_old", "logp_ref")}
+    ref = R.policy(few["logits"], few["target"], few["advantage"], weight=few["weight"], **opt, **kw)
+    bound = 3e-5 * ref["scale"][:, None] + EPS[dtype] * ref["grad"].abs()
+    for b in range(0, T, 61):
+        n = min(61, T - b)
+        err = (got["logp"][b:b + n].double() - ref["logp"][:n]).abs()
+        assert (err <= 1e-5 + 2.0 ** -24 * ref["logp"][:n].abs()).all(), (b, float(err.max()))
+        assert ((got["entropy"][b:b + n].double() - ref["entropy"][:n]).abs() <= 1e-4).all(), b
+        assert ((got["grad"][b:b + n, :V].double() - ref["grad"][:n]).abs() <= bound[:n]).all(), b
+    assert (got["grad"][:, V:] == 7.0).all() and got["status"] == 0
+    # the loss is linear in the weights: each of the 61 rows counts as often as it came
+    times = torch.bincount(which).to(torch.float64)
+    total = R.policy(few["logits"], few["target"], few["advantage"], weight=few["weight"].double() * times, **opt,
+                     **kw)
+    size = float(total["scale"].sum() + total["loss"].abs().sum())
+    assert ((got["loss"].double() - total["loss"]).abs() <= 2e-5 * size).all()
+
+
 @pytest.mark.parametrize("V,ld_grad", [(1000, 1001), (1024, 1040), (333, 334)])
 def test_gradient_rows_of_another_stride(V, ld_grad):
     c = make(6, V, "bf16", V)
