@@ -99,7 +99,8 @@ extern "C" {
 
 size_t pr2_policy_loss_workspace_bytes(const pr2_policy_dims* dims) {
   if (check_policy(dims) != PR2_OK) return 0;
-  return sizeof(double) * 4 * kPolicyParts;
+  const size_t order = dims->T <= kPolicyDealt ? sizeof(int) * static_cast<size_t>(dims->T + 1) : 0;
+  return sizeof(double) * 4 * kPolicyParts + order;
 }
 
 pr2_status pr2_policy_loss(const pr2_policy_dims* dims, const void* logits, const int32_t* target,
@@ -149,6 +150,7 @@ pr2_status pr2_policy_loss(const pr2_policy_dims* dims, const void* logits, cons
   a.entropy = entropy;
   a.grad = grad;
   a.partial = static_cast<double*>(workspace);
+  a.order = reinterpret_cast<int*>(a.partial + 4 * kPolicyParts);
   a.status = status_dev;
   return finish(launch_policy_loss(a, num_sms, st), dm.flags, status_dev, st);
 }

@@ -25,7 +25,7 @@
 // masked tokens: 4096 x 131072 bf16 361 us with the gradient (88 % of the copy rate), 161 without (98 %);
 // 8192 x 32001 178 us (87 %); 2048 x 131072 fp32 349 us (91 %); 32768 x 2048 (warps) 72 us (55 %, the
 // token's arithmetic); one token of 131072 7.3 us.
-// Tokens are dealt to clusters (warps) by their number; each sums its tokens' terms in double and
+// Tokens are dealt to clusters (warps) by their numbers and masks; each sums its tokens' terms in double and
 // policy_finish_kernel the clusters' in order, so the loss does not depend on timing.
 #include <math_constants.h>
 
@@ -510,6 +510,7 @@ constexpr int kTokens = 2;  // token records ahead of the consumers
 
 // A row's token as the producer hands it to the consumers.
 struct TokenRecord {
+  int t;  // T: no more
   float w;
   int target;
   TokenIn in;
@@ -562,6 +563,106 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
   }
 }
 
+// ---- which cluster takes which token ---------------------------------------------------------------
+// Masked tokens take a fraction of the others' time, so with weights both kinds are dealt out evenly.  The
+// first `groups` tokens go to the clusters in order: no row waits for the deal.  The others stand in a list,
+// those that count first, and its first D, D the masked tokens among the first `groups`, go to the clusters
+// that began with those; from there on all take turns.  order: D; [groups] a cluster's place among the D, -1:
+// none; [T - groups] the list.  The deal runs beside the first rows.  us by number / dealt: 4096 x 131072 bf16
+// forward with no token masked 161 / 163, a tenth 157 / 150, half 121 / 89; with the gradient 361 / 363, 357 / 340,
+// 289 / 265; 8192 x 8192 bf16 with the gradient 62.9 / 64.5, 61.3 / 61.7, 52.8 / 45.0.  Beyond kPolicyDealt tokens
+// a cluster's share of the masked ones is even enough by number.
+constexpr int kDealThreads = 1024, kDealVecs = 8;
+
+__global__ void __launch_bounds__(kDealThreads) policy_deal_kernel(const float* weight, int T, int groups,
+                                                                   int* order) {
+  __shared__ int3 warp_sum[32];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int* place = order + 1;
+  int* list = place + groups;
+  int3 all = make_int3(0, 0, 0);  // tokens so far: that count, masked, masked among the first
+  for (int base = 0; base < T; base += kDealThreads * kDealVecs) {
+    const int t0 = base + warp * 32 * kDealVecs + lane;
+    float w[kDealVecs];
+#pragma unroll
+    for (int j = 0; j < kDealVecs; ++j) w[j] = t0 + j * 32 < T ? weight[t0 + j * 32] : 0.f;
+    uint32_t live[kDealVecs], dead[kDealVecs], head[kDealVecs];
+    int3 mine = make_int3(0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < kDealVecs; ++j) {
+      const int t = t0 + j * 32;
+      live[j] = __ballot_sync(0xffffffffu, t >= groups && t < T && w[j] != 0.f);
+      dead[j] = __ballot_sync(0xffffffffu, t >= groups && t < T && w[j] == 0.f);
+      head[j] = __ballot_sync(0xffffffffu, t < groups && w[j] == 0.f);
+      mine.x += __popc(live[j]);
+      mine.y += __popc(dead[j]);
+      mine.z += __popc(head[j]);
+    }
+    __syncthreads();  // (the sums of the tokens before have been read)
+    if (lane == 0) warp_sum[warp] = mine;
+    __syncthreads();
+    int3 s = warp_sum[lane];
+    const int3 own = s;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int x = __shfl_up_sync(0xffffffffu, s.x, o), y = __shfl_up_sync(0xffffffffu, s.y, o);
+      const int z = __shfl_up_sync(0xffffffffu, s.z, o);
+      if (lane >= o) s.x += x, s.y += y, s.z += z;
+    }
+    int l = all.x + __shfl_sync(0xffffffffu, s.x - own.x, warp);
+    int d = all.y + __shfl_sync(0xffffffffu, s.y - own.y, warp);
+    int h = all.z + __shfl_sync(0xffffffffu, s.z - own.z, warp);
+    all.x += __shfl_sync(0xffffffffu, s.x, 31);
+    all.y += __shfl_sync(0xffffffffu, s.y, 31);
+    all.z += __shfl_sync(0xffffffffu, s.z, 31);
+    const uint32_t lower = (1u << lane) - 1u;
+#pragma unroll
+    for (int j = 0; j < kDealVecs; ++j) {
+      const int t = t0 + j * 32;
+      if (live[j] >> lane & 1u) list[l + __popc(live[j] & lower)] = t;
+      if (dead[j] >> lane & 1u) list[T - groups - 1 - (d + __popc(dead[j] & lower))] = t;
+      if (t < groups) place[t] = head[j] >> lane & 1u ? h + __popc(head[j] & lower) : -1;
+      l += __popc(live[j]);
+      d += __popc(dead[j]);
+      h += __popc(head[j]);
+    }
+  }
+  if (threadIdx.x == 0) *order = all.z;
+}
+
+// A cluster's tokens after its first.
+struct Turns {
+  const int* list;  // NULL: by number
+  int T, groups, own, at, n, extra;
+
+  // (behind pdl_wait; through L2, which the deal's stores have reached)
+  __device__ __forceinline__ void begin(const int* order) {
+    if (order == nullptr) {
+      list = nullptr;
+      at = own + groups;
+      return;
+    }
+    list = order + 1 + groups;
+    n = T - groups;
+    extra = __ldcg(order);
+    at = __ldcg(order + 1 + own);
+    if (at < 0) at = extra + own;
+  }
+  __device__ __forceinline__ int next() {  // T: none left
+    if (list == nullptr) {
+      const int t = at < T ? at : T;
+      at = t < T ? t + groups : T;
+      return t;
+    }
+    if (at >= n) return T;
+    const int t = __ldcg(list + at);
+    at = at < extra ? extra + own : at + groups;
+    return t;
+  }
+};
+
 // A CTA's part of a row: `n` vectors from vector v0 on, in `chunks` chunks.
 struct Slice {
   RowShape sh;
@@ -607,7 +708,8 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
     cluster_sync();  // peers arrive here from the first row on
   else
     __syncthreads();
-  pdl_wait();
+  // (with a deal, its kernel has waited for all that came before; the producer waits for the deal itself)
+  if (a.order == nullptr) pdl_wait();
   pdl_trigger();
   const T* logits = static_cast<const T*>(a.logits);
   const bool hold = a.grad != nullptr;
@@ -628,18 +730,34 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
     if (lane == 0) {
       RingAt<kRing> at{0, 0u};
       uint32_t landing = 0, last_round = 0;  // slots with a copy issued, and its round
-      // a token's row number, weight and inputs are loaded two rows ahead, its target's logit one ahead
-      Token cur = load_token(a, first), next = load_token(a, first + groups);
-      TokenIn cur_in = load_inputs(a, first), next_in = load_inputs(a, first + groups);
+      // a token's number is read three rows ahead, its weight and inputs two, its target's logit one
+      const int T_all = static_cast<int>(a.T);
+      const bool dealt = a.order != nullptr;
+      Turns turns{nullptr, T_all, groups, first, 0, 0, 0};
+      Token cur = load_token(a, first), next{T_all, 0.f, 0}, after = next;
+      TokenIn cur_in = load_inputs(a, first), next_in{}, after_in{};
+      int ahead = T_all;
+      auto begin_turns = [&] {
+        turns.begin(a.order);
+        const int t = turns.next();
+        ahead = turns.next();
+        next = load_token(a, t);
+        next_in = load_inputs(a, t);
+      };
+      auto look_ahead = [&] {
+        after = load_token(a, ahead);
+        after_in = load_inputs(a, ahead);
+        ahead = turns.next();
+        check_token(a, next, rank == 0);
+        next_in.za = load_target<T>(a, next);
+      };
+      if (!dealt) begin_turns();
       check_token(a, cur, rank == 0);
       cur_in.za = load_target<T>(a, cur);
       uint32_t row = 0;
       bool ok = true;
-      while (cur.t < a.T && ok) {
-        const Token after = load_token(a, next.t + groups);
-        const TokenIn after_in = load_inputs(a, next.t + groups);
-        check_token(a, next, rank == 0);
-        next_in.za = load_target<T>(a, next);
+      for (;;) {
+        if (row > 0 || !dealt) look_ahead();
         Slice s{};
         const char* src = nullptr;
         int again = 0;
@@ -669,9 +787,15 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
         const int rec = row % kTokens;
         if (ok) ok = mbar_wait(&read[rec], ((row / kTokens) & 1u) ^ 1u, abort_flag, a.status);
         if (!ok) break;
-        record[rec] = TokenRecord{cur.w, cur.target, cur_in};
+        record[rec] = TokenRecord{cur.t, cur.w, cur.target, cur_in};
         mbar_arrive(&told[rec]);
         load_chunks(early, chunks);
+        if (!ok || cur.t >= T_all) break;
+        if (row == 0 && dealt) {
+          pdl_wait();
+          begin_turns();
+          look_ahead();
+        }
         cur = next;
         cur_in = next_in;
         next = after;
@@ -706,11 +830,11 @@ __global__ void __launch_bounds__(32 * (Rows::kWarps + 1), Rows::kCtas)
       return left < kChunkVecs ? left : kChunkVecs;
     };
     bool ok = true;
-    uint32_t turn = 0;
-    for (int t = first; t < a.T; t += groups, ++turn) {
+    for (uint32_t turn = 0;; ++turn) {
       const int rec = turn % kTokens;
       if (!wait(&told[rec], (turn / kTokens) & 1u)) break;
-      const Token cur{t, record[rec].w, record[rec].target};
+      const Token cur{record[rec].t, record[rec].w, record[rec].target};
+      if (cur.t >= a.T) break;
       const Slice sl = slice_of(cur.t);
       // the entries outside whole vectors: threads 0-7 the head's, 8-15 the tail's, of rank 0
       int edge = -1;
@@ -966,12 +1090,20 @@ int active_clusters(int C) {
 
 // Rows over clusters of C CTAs; *parts: the clusters that take rows.
 template <typename T, typename Rows>
-cudaError_t launch_rows(const PolicyArgs& a, int64_t nvec, int C, int64_t* parts, cudaStream_t st) {
+cudaError_t launch_rows(const PolicyArgs& args, int64_t nvec, int C, int64_t* parts, cudaStream_t st) {
+  PolicyArgs a = args;
   int64_t groups = active_clusters<T, Rows>(C);
   if (groups <= 0) return cudaErrorInvalidConfiguration;
   if (groups > a.T) groups = a.T;
   if (groups > kPolicyParts) groups = kPolicyParts;
   *parts = groups;
+  if (a.weight != nullptr && a.T > groups && a.T <= kPolicyDealt) {
+    const cudaError_t err = launch_pdl(policy_deal_kernel, dim3(1), dim3(kDealThreads), 0, st, 1, a.weight,
+                                       static_cast<int>(a.T), static_cast<int>(groups), a.order);
+    if (err != cudaSuccess) return err;
+  } else {
+    a.order = nullptr;
+  }
   return launch_pdl(policy_row_kernel<T, Rows>, dim3(static_cast<unsigned>(groups * C)),
                     dim3(32 * (Rows::kWarps + 1)), ring_bytes<Rows>(), st, C, a, C,
                     static_cast<int>((nvec + C - 1) / C));

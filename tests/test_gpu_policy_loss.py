@@ -136,6 +136,46 @@ def test_long_rows_in_large_batches(dtype, T, V, pad, shift):
     assert ((got["loss"].double() - total["loss"]).abs() <= 2e-5 * size).all()
 
 
+def masks(T, kind):
+    t = torch.arange(T)
+    x = torch.rand(T, generator=torch.Generator().manual_seed(T))
+    return {"none": t >= 0, "all": t < 0, "first half": t >= T // 2, "second half": t < T // 2,
+            "all but the last": t == T - 1, "runs": (t // 100) % 3 != 0, "random": x < 0.4}[kind]
+
+
+@pytest.mark.parametrize("kind", ["none", "all", "first half", "second half", "all but the last", "runs", "random"])
+@pytest.mark.parametrize("dtype,T,V,grad", [
+    ("bf16", 1000, 5001, True), ("fp32", 700, 6500, True), ("bf16", 9001, 4200, True), ("bf16", 65536, 4104, False),
+    ("bf16", 65537, 4104, False)])
+def test_masked_tokens_in_large_batches(dtype, T, V, grad, kind):
+    """Masked tokens and the others reach the CTAs in turns of their own; every token is done once.  61 different
+    rows in turn; a row's gradient and its part of the loss are linear in its weight."""
+    few = make(61, V, dtype, V)
+    few["weight"] = torch.ones(61)
+    which = torch.arange(T) % 61
+    c = {n: few[n][which] for n in ("target", "advantage", "logp_old", "logp_ref")}
+    weight = masks(T, kind) * (0.5 + torch.arange(T) % 7) / T
+    c.update(weight=weight.float(), buf=few["logits"][which].flatten(), shift=0, ld=V, V=V)
+    c["logits"] = c["buf"].view(T, V)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.05)
+    got = call(c, dtype, grad=grad, **kw)
+    opt = {n: few[n] for n in ("weight", "logp_old", "logp_ref")}
+    ref = R.policy(few["logits"], few["target"], few["advantage"], **opt, **kw)
+    w, live = c["weight"].double(), c["weight"] != 0
+    for n, bound in (("logp", 1e-5 + 2.0 ** -24 * ref["logp"].abs()), ("entropy", torch.full((61,), 1e-4))):
+        err = (got[n].double() - torch.where(live, ref[n][which], 0.0)).abs()
+        assert (err <= torch.where(live, bound[which].double(), 0.0)).all(), n
+    total = R.policy(few["logits"], few["target"], few["advantage"], logp_old=few["logp_old"],
+                     logp_ref=few["logp_ref"], weight=torch.bincount(which, w, 61), **kw)
+    size = float(total["scale"].sum() + total["loss"].abs().sum())
+    assert ((got["loss"].double() - total["loss"]).abs() <= 2e-5 * size).all()
+    for b in range(0, T if grad else 0, 61):
+        n = min(61, T - b)
+        want, row = w[b:b + n, None] * ref["grad"][:n], w[b:b + n] * ref["scale"][:n]
+        bound = 3e-5 * row[:, None] + EPS[dtype] * want.abs()
+        assert ((got["grad"][b:b + n].double() - want).abs() <= bound).all(), b
+
+
 @pytest.mark.parametrize("V,ld_grad", [(1000, 1001), (1024, 1040), (333, 334)])
 def test_gradient_rows_of_another_stride(V, ld_grad):
     c = make(6, V, "bf16", V)
