@@ -336,6 +336,48 @@ def test_captured_in_a_graph():
         assert torch.equal(loss.cpu(), want["loss"]) and torch.equal(grad.cpu(), want["grad"])
 
 
+@pytest.mark.parametrize("T,V", [(2, 3000), (5, 40000), (63, 3000), (64, 3000), (65, 3000), (9, 500), (512, 500),
+                                 (513, 500)])
+def test_loss_in_any_workspace_and_in_replays(T, V):
+    """Whatever the workspace holds, one call after another, and a graph replayed with other weights."""
+    c = make(T, V, "bf16", T + V)
+    dm = B.policy_dims(T, V, "bf16", kl_coef=0.05)
+    opt = {n: c[n].cuda() for n in ("logits", "target", "weight", "advantage", "logp_old", "logp_ref")}
+    opt["weight"][:] = 1.0 / T
+    loss = torch.full((4,), math.nan, device="cuda")
+    ws = B.alloc_policy_workspace(dm)
+
+    def run():
+        B.check(B.pr2_policy_loss(dm, opt["logits"], opt["target"], opt["weight"], opt["advantage"], opt["logp_old"],
+                                  opt["logp_ref"], loss, None, None, None, ws))
+
+    ref = R.policy(c["logits"], c["target"], c["advantage"], logp_old=c["logp_old"], logp_ref=c["logp_ref"],
+                   weight=torch.full((T,), 1.0 / T), kl_coef=0.05)
+    size = float(ref["scale"].sum() + ref["loss"].abs().sum())
+
+    def right(factor):
+        off = (loss.cpu().double() / factor - ref["loss"]).abs()
+        assert (off <= 2e-5 * size).all(), (factor, off)
+
+    for i in range(50):
+        ws.fill_(i)
+        loss.fill_(math.nan)
+        run()
+        right(1.0)
+    for i in range(50):
+        loss.fill_(math.nan)
+        run()
+        right(1.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for i in range(50):
+        opt["weight"][:] = 2.0 ** (i % 5) / T
+        loss.fill_(math.nan)
+        graph.replay()
+        right(2.0 ** (i % 5))
+
+
 def test_gradient_against_differences_of_the_loss():
     """fp32 differences: loss errors 2e-5 of the terms' size over a step of 2^-6 give 3e-3 of it, the
     step's own error is below 2^-12 of it."""
