@@ -146,7 +146,7 @@ def masks(T, kind):
 @pytest.mark.parametrize("kind", ["none", "all", "first half", "second half", "all but the last", "runs", "random"])
 @pytest.mark.parametrize("dtype,T,V,grad", [
     ("bf16", 1000, 5001, True), ("fp32", 700, 6500, True), ("bf16", 9001, 4200, True), ("bf16", 65536, 4104, False),
-    ("bf16", 65537, 4104, False)])
+    ("bf16", 65537, 4104, False), ("bf16", 1400, 52001, False), ("fp32", 600, 30000, False), ("fp32", 3000, 9001, False)])
 def test_masked_tokens_in_large_batches(dtype, T, V, grad, kind):
     """Masked tokens and the others reach the CTAs in turns of their own; every token is done once.  61 different
     rows in turn; a row's gradient and its part of the loss are linear in its weight."""
