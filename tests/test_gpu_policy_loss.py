@@ -146,7 +146,8 @@ def masks(T, kind):
 @pytest.mark.parametrize("kind", ["none", "all", "first half", "second half", "all but the last", "runs", "random"])
 @pytest.mark.parametrize("dtype,T,V,grad", [
     ("bf16", 1000, 5001, True), ("fp32", 700, 6500, True), ("bf16", 9001, 4200, True), ("bf16", 65536, 4104, False),
-    ("bf16", 65537, 4104, False), ("bf16", 1400, 52001, False), ("fp32", 600, 30000, False), ("fp32", 3000, 9001, False)])
+    ("bf16", 65537, 4104, False), ("bf16", 1400, 52001, False), ("fp32", 600, 30000, False),
+    ("fp32", 3000, 9001, False)])
 def test_masked_tokens_in_large_batches(dtype, T, V, grad, kind):
     """Masked tokens and the others reach the CTAs in turns of their own; every token is done once.  61 different
     rows in turn; a row's gradient and its part of the loss are linear in its weight."""
@@ -376,6 +377,49 @@ def test_loss_in_any_workspace_and_in_replays(T, V):
         loss.fill_(math.nan)
         graph.replay()
         right(2.0 ** (i % 5))
+
+
+@pytest.mark.parametrize("T,V,grad", [(1000, 5000, True), (1300, 52000, True), (2000, 9000, False), (40, 5000, True)])
+def test_calls_follow_what_is_before_them_in_the_stream(T, V, grad):
+    """Logits and weights written right before a call, a call right behind another with the same workspace, its
+    outputs read and its inputs overwritten right after: the same bits as each call alone."""
+    c = make(T, V, "bf16", T)
+    base = c["logits"].cuda()
+    names = ("target", "weight", "advantage", "logp_old", "logp_ref")
+    opt = {n: c[n].cuda() for n in names}
+    dm = B.policy_dims(T, V, "bf16", kl_coef=0.05)
+    ws = B.alloc_policy_workspace(dm)
+    z, w, g = torch.zeros_like(base), torch.zeros_like(opt["weight"]), torch.zeros_like(base) if grad else None
+    loss = [torch.zeros(4, device="cuda") for _ in range(2)]
+    logp = torch.zeros(T, device="cuda")
+    weights = [opt["weight"], opt["weight"].flip(0).contiguous()]
+
+    def run(i):
+        B.check(B.pr2_policy_loss(dm, z, opt["target"], w, opt["advantage"], opt["logp_old"], opt["logp_ref"],
+                                  loss[i % 2], logp, None, g, ws))
+
+    alone = []
+    for i in range(2):
+        z.copy_(base)
+        w.copy_(weights[i])
+        torch.cuda.synchronize()
+        run(i)
+        torch.cuda.synchronize()
+        alone.append([loss[i].clone(), logp.clone(), g.clone() if grad else None])
+    seen = []
+    for i in range(30):
+        z.fill_(-3.0)
+        w.fill_(7.0)
+        torch.mul(base, 1.0, out=z)
+        w.copy_(weights[i % 2])
+        run(i)
+        run(i)
+        seen.append([loss[i % 2].clone(), logp.clone(), g.clone() if grad and i > 27 else None])
+    torch.cuda.synchronize()
+    for i, got in enumerate(seen):
+        want = alone[i % 2]
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+        assert got[2] is None or torch.equal(got[2], want[2]), i
 
 
 def test_gradient_against_differences_of_the_loss():
