@@ -10,8 +10,8 @@
 // Exponentials are powers of two of logit scale - M, scale = inv_temp log2 e, one fused operation.  A
 // sum of positive terms is as exact relative to any M that neither overflows nor loses it, so M is 0
 // to begin with and is set to the entries' maximum (rounded: it shifts l and the target's term alike)
-// only where the sums over- or underrun it.  Where M itself would overflow (a row at the type's lowest
-// value) the difference logit - m is taken first.
+// only where the sums over- or underrun it.  Where M would be too large to keep its fraction (a row at a
+// large mask value) the difference logit - m is taken first.
 //
 // A row is read from HBM once.  A producer warp streams it, by bulk copies, through a ring of chunks
 // in shared memory, and the chunks that fit stay there between the passes.  Of a longer row the first
@@ -130,24 +130,28 @@ struct RowSum {
   float m = 0.f, l = 0.f, e = 0.f;
 };
 
-// M(m) is m scale in 32 bits, unless that is too large to be subtracted safely: then NaN, and
-// y = (logit - m) scale.
+// M(m) is m scale in 32 bits while its rounding, which moves every y by as much, stays below 2^-4.  Beyond
+// that (finite mask values among them: at -1e10 m scale - M may be 440, whose power is infinite) it is NaN,
+// and y = (logit - m) scale.
+constexpr float kMostRef = 1048576.f;  // 2^20
 __device__ __forceinline__ float scaled_ref(float m, float scale) {
   const float M = m * scale;
-  return fabsf(M) <= 1e37f ? M : __uint_as_float(0x7fc00000u);
+  return fabsf(M) <= kMostRef ? M : __uint_as_float(0x7fc00000u);
 }
 __device__ __forceinline__ float power_of(float z, float m, float M, float scale) {
   return M == M ? fmaf(z, scale, -M) : (z - m) * scale;
 }
 
-// The sums relative to another logit.
+// The sums relative to another logit.  (The gap is between what was subtracted and what is to be: the
+// rounded M where there is one, else the product itself.)
 __device__ __forceinline__ void raise(RowSum& s, float m, float scale) {
   if (s.m == m || s.l == 0.f) {
     s.m = m;
     return;
   }
   const float from = scaled_ref(s.m, scale), to = scaled_ref(m, scale);
-  const float gap = from == from && to == to ? from - to : (s.m - m) * scale;
+  const float gap = from == from ? (to == to ? from - to : fmaf(-m, scale, from))
+                                 : (to == to ? fmaf(s.m, scale, -to) : (s.m - m) * scale);
   const float f = exp2_approx(gap);
   s.e = f == 0.f ? s.l * f : fmaf(gap, s.l, s.e) * f;
   s.l *= f;
@@ -335,7 +339,7 @@ __device__ __forceinline__ void grad_span(Load load, T* out, int n, int tid, con
                                           int at) {
   constexpr int E = Vec<T>::kElems;
   if ((reinterpret_cast<uintptr_t>(out) & 15u) != 0 || (g.f != 0.f && g.M != g.M)) {
-    // rows of another alignment than the logits', rows whose M overflows
+    // rows of another alignment than the logits', rows without an M
     for (int v = tid; v < n; v += kStride) {
       const uint4 w = g.f != 0.f ? load(v) : make_uint4(0u, 0u, 0u, 0u);
       const T* e = reinterpret_cast<const T*>(&w);
