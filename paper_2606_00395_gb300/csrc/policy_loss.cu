@@ -163,7 +163,7 @@ __device__ __forceinline__ void add_one(RowSum& s, float z, float scale) {
   if (z > s.m || s.l == 0.f) raise(s, z, scale);
   const float y = power_of(z, s.m, scaled_ref(s.m, scale), scale), p = exp2_approx(y);
   s.l += p;
-  s.e = fmaf(p, y, s.e);
+  s.e = p != 0.f ? fmaf(p, y, s.e) : s.e;  // (y may be -inf)
 }
 
 // Vectors src[v], src[v + stride], ... below n, kVecs of them at most, relative to their maximum or

@@ -69,3 +69,17 @@ def test_rows_far_from_zero(V, offset):
     c["logp_old"], c["logp_ref"] = (lp - 0.05).float(), (lp + 0.1).float()
     kw = dict(kl_coef=0.05)
     check(c, call(c, "fp32", **kw), "fp32", **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("inv_temp", [0.7, 1.0, 1.3])
+@pytest.mark.parametrize("T,V,shift", [(6, 21, 1), (6, 301, 3), (6, 999, 1), (6, 5003, 1), (6, 32001, 5), (500, 5003, 0)])
+def test_first_and_last_entries_at_the_lowest_value(T, V, shift, inv_temp, dtype):
+    """Only a few entries at either end, most of them outside the row's whole vectors."""
+    v = torch.arange(V)
+    mask = ((v < 3) | (v >= V - 3)).expand(T, V)
+    value = torch.finfo(DT[dtype]).min
+    c = masked(T, V, dtype, V, mask, value, shift, inv_temp=inv_temp)
+    # (a target at either end keeps its logit, so the others of that end are the masked ones)
+    kw = dict(clip_high=0.28, kl_coef=0.05, inv_temp=inv_temp)
+    check(c, call(c, dtype, **kw), dtype, **kw)
