@@ -2,11 +2,12 @@
 //
 // gates_s = rho_{idx_s} of rho = Softmax(p), so with dr_j = sum of dgates over the slots that name
 // expert j:  dp_j = rho_j (dr_j - G),  G = sum_s dgates_s rho_{idx_s}.
-// Renormalised gates g_s = rho_{idx_s} / S:  d rho_{idx_s} = (dgates_s - sum_u dgates_u g_u) / S =: dr,
-// and G = sum dr rho = 0 exactly, so only the selected experts get a gradient, g_s (dgates_s - G').
+// Renormalised gates g_s = rho_{idx_s} / S:  only the selected experts get a gradient,
+// g_s (dgates_s - G'),  G' = sum_s dgates_s g_s:  the same form with g_s for rho.  (S may be a denormal number
+// where the replayed experts have all but vanished; the gates are finite all the same.)
 // 8, 16 or 32 lanes per token, lane s holding slot s, four experts a lane and step: every expert's -rho_j G is
-// stored first, then the selected ones' values over it.  N not a multiple of 4: a warp per token with dr
-// in shared memory.  Bound by HBM for large batches (rho read, dp written): 262144 x 256 with
+// stored first, then the selected ones' values over it.  N not a multiple of 4: a warp per token, an expert
+// a lane and step.  Bound by HBM for large batches (rho read, dp written): 262144 x 256 with
 // k = 8 91 us (90 % of the copy rate), 10^6 x 64 with k = 4 117 us (68 %); 4096 x 128 with k = 8
 // is 4.5 MB and takes 4.4 us a call, the host's part.
 #include "pr2_device.cuh"
@@ -17,14 +18,37 @@ namespace {
 
 constexpr int kWarps = 8;
 
-// Sums over a token's kLanes lanes.
+// Sum over a token's kLanes lanes.
 template <int kLanes>
-__device__ __forceinline__ void token_sums(float& a, float& b) {
+__device__ __forceinline__ float token_sum(float v) {
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// A slot's probability (0: no slot) becomes its gate; returns G.  Renormalised, with S = 0 giving gates of 0 and
+// a NaN going through: both sums go round together and take one reciprocal, of S 2^64 where S is small and 1 / S
+// may overflow (10^6 x 64, k = 4 119 us; rho / S and G / S as two divisions 136).  There the products with
+// dgates may be denormal numbers, and G is summed again from the gates.
+constexpr float kSmallSum = 9.0949470e-13f, kUp = 18446744073709551616.f;  // 2^-40, 2^64
+template <int kLanes>
+__device__ __forceinline__ float gates_and_mean(float& rho, float dg, int norm) {
+  float G = dg * rho;
+  if (!norm) return token_sum<kLanes>(G);
+  float S = rho;
 #pragma unroll
   for (int o = kLanes / 2; o > 0; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b += __shfl_xor_sync(0xffffffffu, b, o);
+    G += __shfl_xor_sync(0xffffffffu, G, o);
+    S += __shfl_xor_sync(0xffffffffu, S, o);
   }
+  const float up = S < kSmallSum ? kUp : 1.f, inv = S == 0.f ? 0.f : 1.f / (S * up);
+  rho = rho * up * inv;
+  G *= inv;
+  if (__any_sync(0xffffffffu, S < kSmallSum)) {
+    const float again = token_sum<kLanes>(dg * rho);
+    if (S < kSmallSum) G = again;
+  }
+  return G;
 }
 
 // N % 4 == 0, N <= 16 kLanes, k <= kLanes; rows on 16 bytes.
@@ -53,7 +77,7 @@ __global__ void __launch_bounds__(kWarps * 32)
     const int e = next_e;
     float dg = next_dg;
     bool ok = e >= 0 && e < N;
-    float rho = ok ? probs[t * N + e] : 0.f;
+    float gate = ok ? probs[t * N + e] : 0.f;
     float4 r[kSteps];
     const float4* row = reinterpret_cast<const float4*>(probs + t * N);
 #pragma unroll
@@ -65,20 +89,15 @@ __global__ void __launch_bounds__(kWarps * 32)
       if (s < sub && other == e) ok = false;
     }
     if (live && sub < k && !ok && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
-    if (!ok) dg = rho = 0.f;
-    float G = dg * rho, S = rho;
-    token_sums<kLanes>(G, S);
-    if (norm) {
-      dg = S > 0.f ? (dg - G / S) / S : 0.f;
-      G = 0.f;
-    }
+    if (!ok) dg = gate = 0.f;
+    const float G = gates_and_mean<kLanes>(gate, dg, norm), others = norm ? 0.f : -G;
     float4* out = reinterpret_cast<float4*>(dlogits + t * N);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
       if (live && sub + i * kLanes < vecs)
-        out[sub + i * kLanes] = make_float4(-G * r[i].x, -G * r[i].y, -G * r[i].z, -G * r[i].w);
+        out[sub + i * kLanes] = make_float4(others * r[i].x, others * r[i].y, others * r[i].z, others * r[i].w);
     __syncwarp();  // (the selected ones' values come after)
-    if (ok) dlogits[t * N + e] = rho * (dg - G);
+    if (ok) dlogits[t * N + e] = gate * (dg - G);
   }
 }
 
@@ -86,39 +105,25 @@ __global__ void __launch_bounds__(kWarps * 32)
     gates_backward_any_kernel(const float* __restrict__ probs, const int32_t* __restrict__ idx,
                           const float* __restrict__ dgates, int64_t T, int N, int k, int norm,
                           float* __restrict__ dlogits, int32_t* __restrict__ status) {
-  __shared__ float dr_s[kWarps][kMaxExperts];
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
-  float* dr = dr_s[threadIdx.x >> 5];
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5); t < T;
        t += static_cast<int64_t>(gridDim.x) * kWarps) {
     const int e = lane < k ? idx[t * k + lane] : -1;
     float dg = lane < k ? dgates[t * k + lane] : 0.f;
-    for (int j = lane; j < N; j += 32) dr[j] = 0.f;
     bool ok = lane < k && e >= 0 && e < N;
     for (int s = 0; s < k - 1; ++s) {
       const int other = __shfl_sync(0xffffffffu, e, s);
       if (s < lane && other == e) ok = false;
     }
     if (lane < k && !ok && status != nullptr) atomicOr(status, PR2_STATUS_BAD_INDEX);
-    const float rho = ok ? probs[t * N + e] : 0.f;
     if (!ok) dg = 0.f;
-    float G = dg * rho, S = rho;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      G += __shfl_xor_sync(0xffffffffu, G, o);
-      S += __shfl_xor_sync(0xffffffffu, S, o);
-    }
-    if (norm) {
-      dg = S > 0.f ? (dg - G / S) / S : 0.f;
-      G = 0.f;
-    }
-    __syncwarp();
-    if (ok) dr[e] = dg;
-    __syncwarp();
-    for (int j = lane; j < N; j += 32) dlogits[t * N + j] = probs[t * N + j] * (dr[j] - G);
-    __syncwarp();
+    float gate = ok ? probs[t * N + e] : 0.f;
+    const float G = gates_and_mean<32>(gate, dg, norm), others = norm ? 0.f : -G;
+    for (int j = lane; j < N; j += 32) dlogits[t * N + j] = others * probs[t * N + j];
+    __syncwarp();  // (the selected ones' values come after)
+    if (ok) dlogits[t * N + e] = gate * (dg - G);
   }
 }
 
