@@ -41,6 +41,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2Rest = static_cast<float>(0.6931471805599453 - static_cast<double>(kLn2));
 
 // ---- packed pairs of fp32 -------------------------------------------------------------------
 __device__ __forceinline__ uint64_t pack2(float lo, float hi) {
@@ -436,9 +437,9 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   const float mean = s.e / s.l;
   const float M = scaled_ref(s.m, scale);
   // The target's y, and in `slip` what log 2 times it lacks: the rest of its product and differences,
-  // and to first order what rounding scale and log 2 to 32 bits did to every y (the same to all tokens,
-  // so that it would not average out in the loss): scale_slip moves a y by its own multiple, log l by
-  // that of the mean y.  l = 2^n part with 1 <= part < 2, so logp = (y - n) log 2 - log part, and its
+  // and what rounding scale and log 2 to 32 bits did (the same to all tokens, so that it would not average
+  // out in the loss): to first order scale_slip moves a y by its own multiple, log l by that of the mean
+  // y, and log 2 is a factor of y - n.  l = 2^n part with 1 <= part < 2, so logp = (y - n) log 2 - log part, and its
   // distance from another log-probability x is taken as one fused product less x: the ratio does not
   // lose what the logarithm of a large l would.  (A NaN or infinity stays in part; an infinite y, a
   // target that is banned, has no rest.)
@@ -452,7 +453,7 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
     const float back = y - p, back_n = yn - y;
     float rest = (y - (yn - back_n)) - (nf + back_n);
     if (M == M) rest += fmaf(in.za, scale, -p) + ((p - (y - back)) - (M + back));
-    slip = fmaf(rest, kLn2, fmaf(y, a.log_slip, -a.scale_slip * mean));
+    slip = fmaf(rest, kLn2, fmaf(yn, kLn2Rest, a.scale_slip * (y - mean)));
   }
   auto logp_less = [&](float x) { return fmaf(yn, kLn2, -x) - log_part + slip; };
   const float logp = logp_less(0.f);
@@ -1172,11 +1173,9 @@ int grad_cluster(int64_t T, int64_t nvec, int num_sms, int64_t bytes) {
 template <typename T>
 cudaError_t launch(const PolicyArgs& args, int num_sms, cudaStream_t st) {
   PolicyArgs a = args;
-  const double exact = static_cast<double>(a.inv_temp) * 1.4426950408889634, log2 = 0.6931471805599453;
+  const double exact = static_cast<double>(a.inv_temp) * 1.4426950408889634;
   a.scale = static_cast<float>(exact);
-  const double slip = exact / a.scale - 1.0;
-  a.scale_slip = static_cast<float>(log2 * slip);
-  a.log_slip = static_cast<float>(log2 * (1.0 + slip) - static_cast<double>(kLn2));
+  a.scale_slip = static_cast<float>(0.6931471805599453 * (exact / a.scale - 1.0));
   constexpr int E = Vec<T>::kElems;
   const int64_t nvec = a.V / E;  // most whole vectors of a row
   const int64_t resident = static_cast<int64_t>(num_sms) * WideRows::kCtas;

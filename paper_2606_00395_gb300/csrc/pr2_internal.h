@@ -232,7 +232,7 @@ struct PolicyArgs {
   int64_t T, V, ld_logits, ld_grad;
   int bf16;
   float inv_temp, clip_low, clip_high, kl_coef, grad_scale;
-  float scale, scale_slip, log_slip;  // inv_temp log2 e and corrections (set by the launcher)
+  float scale, scale_slip;  // inv_temp log2 e and its rounding's correction (set by the launcher)
   const void* logits;
   const int32_t* target;
   const float *weight, *advantage, *logp_old, *logp_ref;  // nullable: weight, logp_old, logp_ref
