@@ -7,10 +7,11 @@
 // depend on the target's log-probability alone, so a second pass over the row writes
 //   grad_v = f [v = a] - (f / l) exp(z_v - m),  f = grad_scale inv_temp c
 // (not exp(z - lse): where the row's values are large, lse = m + log l rounds to m).
-// Exponentials are powers of two of logit scale - M, scale = inv_temp log2 e, one fused operation.  A
-// sum of positive terms is as exact relative to any M that neither overflows nor loses it, so M is 0
-// to begin with and is set to the entries' maximum (rounded: it shifts l and the target's term alike)
-// only where the sums over- or underrun it.  Where M would be too large to keep its fraction (a row at a
+// Exponentials are powers of two of y = logit scale - M, scale = inv_temp log2 e, one fused operation.  Its
+// rounding moves a term by up to 2^-25 |y| log 2, 1.3e-6 at the |y| of 40 to 64 that an M of 0 allows, and a
+// logit of nothing like that does not need its row's maximum first: so M is 0 to begin with and is set to
+// the entries' maximum (rounded: it shifts l and the target's term alike) only where the sums over- or
+// underrun it.  Where M would be too large to keep its fraction (a row at a
 // large mask value) the difference logit - m is taken first.
 //
 // A row is read from HBM once.  A producer warp streams it, by bulk copies, through a ring of chunks
@@ -436,7 +437,8 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   }
   const float mean = s.e / s.l;
   const float M = scaled_ref(s.m, scale);
-  // The target's y, and in `slip` what log 2 times it lacks: the rest of its product and differences,
+  // The target's y, as the sums took it, and in `slip` what log 2 times it lacks: the rest of its product and
+  // differences, less what its own power in l has of that (an l that is mostly the target's moves with it),
   // and what rounding scale and log 2 to 32 bits did (the same to all tokens, so that it would not average
   // out in the loss): to first order scale_slip moves a y by its own multiple, log l by that of the mean
   // y, and log 2 is a factor of y - n.  l = 2^n part with 1 <= part < 2, so logp = (y - n) log 2 - log part, and its
@@ -446,20 +448,24 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   const uint32_t bits = __float_as_uint(s.l);
   const int n = bits < 0x7f800000u ? static_cast<int>(bits >> 23) - 127 : 0;
   const float log_part = logf(__uint_as_float(bits - (static_cast<uint32_t>(n) << 23)));
-  const float p = in.za * scale, nf = static_cast<float>(n);
-  const float y = M == M ? p - M : (in.za - s.m) * scale, yn = y - nf;
+  const float nf = static_cast<float>(n), y = power_of(in.za, s.m, M, scale), yn = y - nf;
   float slip = 0.f;
   if (fabsf(y) < CUDART_INF_F) {
-    const float back = y - p, back_n = yn - y;
+    const float back_n = yn - y;
     float rest = (y - (yn - back_n)) - (nf + back_n);
-    if (M == M) rest += fmaf(in.za, scale, -p) + ((p - (y - back)) - (M + back));
+    if (M == M) {
+      const float p = in.za * scale, d = p - M, back = d - p;
+      const float lacks = (d - y) + ((p - (d - back)) - (M + back)) + fmaf(in.za, scale, -p);
+      rest = fmaf(lacks, 1.f - __fdividef(exp2_approx(y), s.l), rest);
+    }
     slip = fmaf(rest, kLn2, fmaf(yn, kLn2Rest, a.scale_slip * (y - mean)));
   }
   auto logp_less = [&](float x) { return fmaf(yn, kLn2, -x) - log_part + slip; };
   const float logp = logp_less(0.f);
-  if (write) {
-    if (a.logp != nullptr) a.logp[k.t] = logp;
-    if (a.entropy != nullptr) a.entropy[k.t] = fmaf(kLn2, nf - mean, log_part);
+  if (write) {  // (no log-probability is above 0, no entropy below; a NaN stays one)
+    if (a.logp != nullptr) a.logp[k.t] = logp > 0.f ? 0.f : logp;
+    const float entropy = fmaf(kLn2, nf - mean, log_part);
+    if (a.entropy != nullptr) a.entropy[k.t] = entropy < 0.f ? 0.f : entropy;
   }
   const float A = in.A;
   const float r = a.logp_old != nullptr ? expf(logp_less(in.old)) : 1.f;
