@@ -461,7 +461,9 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
     slip = fmaf(rest, kLn2, fmaf(yn, kLn2Rest, a.scale_slip * (y - mean)));
   }
   auto logp_less = [&](float x) { return fmaf(yn, kLn2, -x) - log_part + slip; };
-  const float logp = logp_less(0.f);
+  // (a finite logit may be infinite as a multiple of log 2; of l only a NaN counts beside it)
+  const float far = (M == M ? in.za : in.za - s.m) * a.inv_temp - log_part;
+  const float logp = y == -CUDART_INF_F ? far : logp_less(0.f);
   if (write) {  // (no log-probability is above 0, no entropy below; a NaN stays one)
     if (a.logp != nullptr) a.logp[k.t] = logp > 0.f ? 0.f : logp;
     const float entropy = fmaf(kLn2, nf - mean, log_part);

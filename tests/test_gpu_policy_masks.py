@@ -1,5 +1,7 @@
 """Policy loss of rows whose masked entries hold large finite numbers, against the plain 64-bit form
 (tolerances as in test_gpu_policy_loss)."""
+import math
+
 import pytest
 import torch
 
@@ -83,3 +85,18 @@ def test_first_and_last_entries_at_the_lowest_value(T, V, shift, inv_temp, dtype
     # (a target at either end keeps its logit, so the others of that end are the masked ones)
     kw = dict(clip_high=0.28, kl_coef=0.05, inv_temp=inv_temp)
     check(c, call(c, dtype, **kw), dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [300, 9001])
+def test_a_target_at_the_lowest_value(V, dtype):
+    """Its log-probability is that number, which is finite although its multiple by log2 e is not."""
+    c = make(4, V, dtype, 9, std=1.0)
+    c["weight"][:] = 0.25
+    c["advantage"][:] = torch.tensor([1.0, -1.0, 2.0, 0.0])
+    for t in (1, 2, 3):
+        c["logits"][t, c["target"][t].long()] = torch.finfo(DT[dtype]).min
+    got = call(c, dtype, names=("weight", "logp_old"))
+    assert torch.isfinite(got["logp"]).all() and not got["grad"][1:].any()
+    check(c, got, dtype, names=("weight", "logp_old"))
+    assert math.isclose(float(got["logp"][1]), torch.finfo(DT[dtype]).min, rel_tol=1e-6)
