@@ -583,14 +583,22 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
 }
 
 // ---- which cluster takes which token ---------------------------------------------------------------
-// Masked tokens take a fraction of the others' time, so with weights both kinds are dealt out evenly.  The
-// first `groups` tokens go to the clusters in order: no row waits for the deal.  The others stand in a list,
-// those that count first, and its first D, D the masked tokens among the first `groups`, go to the clusters
-// that began with those; from there on all take turns.  order: D; [groups] a cluster's place among the D, -1:
-// none; [T - groups] the list.  The deal runs beside the first rows.  us by number / dealt: 4096 x 131072 bf16
-// forward with no token masked 161 / 163, a tenth 157 / 150, half 121 / 89; with the gradient 361 / 363, 357 / 340,
-// 289 / 265; 8192 x 8192 bf16 with the gradient 62.9 / 64.5, 61.3 / 61.7, 52.8 / 45.0.  Beyond kPolicyDealt tokens
-// a cluster's share of the masked ones is even enough by number.
+// Masked tokens take a fraction of the others' time, so with weights both kinds are dealt out evenly where that
+// pays.  The first `groups` tokens go to the clusters in order: a cluster's first row is asked for before the
+// deal is read.  The others stand in a list, those that count first, and its first D, D the masked tokens among
+// the first `groups`, go to the clusters that began with those; from there on all take turns.  order: D;
+// [groups] a cluster's place among the D, -1: none; [T - groups] the list.
+// The deal is a launch in front of the rows, which wait for it (1 to 3 us), and reading the list costs each row
+// something, so it is made for long rows in batches of some size only (deals).  us by number / dealt, with none, a
+// tenth, three tenths and half of the tokens masked:
+//   gradient, bf16  4096 x 131072 367/369 361/343 328/305 289/267    8192 x 32001 178/180 175/168 175/148 158/137
+//                   32768 x 16384 369/380 350/351 310/307 296/271    1200 x 32001 39.2/41.2 37.6/40.0 35.5/35.1 32.7/32.2
+//                   8192 x 8192 60.9/64.5 60.0/60.5 56.2/53.0 51.1/45.9   65536 x 16384 727/748 691/695 607/607 561/538
+//   forward, bf16   4096 x 131072 163/168 156/150 138/120 114/91     8192 x 50001 134/138 131/126 123/103 100/79
+//                   1500 x 131072 66.5/71.3 64.2/65.5 61.3/53.3 55.7/45.7
+//                   2048 x 65000 49.1/54.0 48.2/50.1 45.0/43.3 41.6/35.5
+//                   16384 x 16384 100/107 96/99 86/83 71/69    65536 x 32000 654/675 612/615 507/499 393/381
+//   forward, fp32   8192 x 32768 162/166 149/152 123/122 91/93       2400 x 32001 53.6/58.2 50.1/53.4 42.1/44.0 35.8/34.7
 constexpr int kDealThreads = 1024, kDealVecs = 8;
 
 __global__ void __launch_bounds__(kDealThreads) policy_deal_kernel(const float* weight, int T, int groups,
@@ -656,7 +664,6 @@ struct Turns {
   const int* list;  // NULL: by number
   int T, groups, own, at, n, extra;
 
-  // (behind pdl_wait; through L2, which the deal's stores have reached)
   __device__ __forceinline__ void begin(const int* order) {
     if (order == nullptr) {
       list = nullptr;
@@ -733,8 +740,7 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
     cluster_sync();  // peers arrive here from the first row on
   else
     __syncthreads();
-  // (with a deal, its kernel has waited for all that came before; the producer waits for the deal itself)
-  if (a.order == nullptr) pdl_wait();
+  pdl_wait();
   pdl_trigger();
   const T* logits = static_cast<const T*>(a.logits);
   const int groups = static_cast<int>(gridDim.x) / C, first = static_cast<int>(blockIdx.x) / C;
@@ -856,7 +862,6 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
         load_chunks(early, chunks);
         if (!ok || cur.t >= T_all) break;
         if (row == 0 && dealt) {
-          pdl_wait();
           begin_turns();
           look_ahead();
         }
@@ -1142,6 +1147,14 @@ int active_clusters(int C) {
   return n;
 }
 
+// Whether the deal pays (figures at policy_deal_kernel).
+bool deals(const PolicyArgs& a, int64_t nvec, int64_t groups) {
+  const bool grad = a.grad != nullptr;
+  const int64_t row = nvec * 16;  // bytes
+  return a.weight != nullptr && a.T > groups && a.T <= kPolicyDealt && row >= (grad ? 32 << 10 : 64 << 10) &&
+         a.T * row >= (grad ? 100000000 : 350000000);
+}
+
 // Rows over clusters of C CTAs; *parts: the clusters that take rows.
 template <typename T, typename Rows, bool kGrad>
 cudaError_t launch_rows(const PolicyArgs& args, int64_t nvec, int C, int64_t* parts, cudaStream_t st) {
@@ -1151,7 +1164,7 @@ cudaError_t launch_rows(const PolicyArgs& args, int64_t nvec, int C, int64_t* pa
   if (groups > a.T) groups = a.T;
   if (groups > kPolicyParts) groups = kPolicyParts;
   *parts = groups;
-  if (a.weight != nullptr && a.T > groups && a.T <= kPolicyDealt) {
+  if (deals(a, nvec, groups)) {
     const cudaError_t err = launch_pdl(policy_deal_kernel, dim3(1), dim3(kDealThreads), 0, st, 1, a.weight,
                                        static_cast<int>(a.T), static_cast<int>(groups), a.order);
     if (err != cudaSuccess) return err;

@@ -244,7 +244,7 @@ struct PolicyArgs {
   int32_t* status;        // nullable
 };
 constexpr int kPolicyParts = 4096;   // most groups of CTAs that sum tokens of their own
-constexpr int kPolicyDealt = 65536;  // most tokens that are dealt out by weight
+constexpr int kPolicyDealt = 32768;  // most tokens that are dealt out by weight
 cudaError_t launch_policy_loss(const PolicyArgs& a, int num_sms, cudaStream_t st);
 
 // ---- tokens sorted by expert, and back (token_sort.cu) -------------------------------------
