@@ -345,6 +345,8 @@ typedef struct {
  *  -inf has no distribution: it contributes nothing, its logp is -inf, its entropy and gradient 0.
  *  A target outside [0, V) sets PR2_STATUS_BAD_INDEX and counts as a token of weight 0.
  *  T = 0 writes loss 0.  fp32 arithmetic, the gradient rounded once.  Deterministic.
+ *  A bounded wait that runs out, in this call or (PR2_STATUS_TIMEOUT in status_dev) before it, makes
+ *  loss NaN, with or without a status word; the other outputs are unspecified then.
  *  workspace: pr2_policy_loss_workspace_bytes(dims) bytes (0: invalid dims), 256-byte aligned.
  */
 size_t pr2_policy_loss_workspace_bytes(const pr2_policy_dims* dims);

@@ -495,6 +495,11 @@ __device__ __forceinline__ RowGrad finish_token(const PolicyArgs& a, const Token
   return g;
 }
 
+__device__ __forceinline__ void spoil(double (&s)[3], bool timed_out) {
+  if (timed_out)
+#pragma unroll
+    for (int j = 0; j < 3; ++j) s[j] = CUDART_NAN;
+}
 __device__ __forceinline__ void write_loss(const PolicyArgs& a, const double (&s)[3]) {
   a.loss[0] = static_cast<float>(a.kl_coef > 0.f ? s[0] + a.kl_coef * s[1] : s[0]);
 #pragma unroll
@@ -552,6 +557,9 @@ __device__ __forceinline__ void arrive_cluster(uint64_t* bar, uint32_t rank) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
                    mapa_shared(smem_u32(bar), rank))
                : "memory");
+}
+__device__ __forceinline__ void st_cluster(int* shared, uint32_t rank, int v) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(mapa_shared(smem_u32(shared), rank)), "r"(v) : "memory");
 }
 __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
@@ -785,7 +793,9 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
     if (a.logp != nullptr) a.logp[t] = 0.f;
     if (a.entropy != nullptr) a.entropy[t] = 0.f;
   };
-  auto store_sums = [&](const double (&sums)[3]) {
+  // Where a wait ran out the sums are NaN: those of the tokens done by then would pass for all of them.
+  auto store_sums = [&](double (&sums)[3]) {
+    spoil(sums, *abort_flag);
     if (groups == 1) {
       write_loss(a, sums);
     } else {
@@ -804,6 +814,7 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
       const int T_all = static_cast<int>(a.T);
       const bool dealt = a.order != nullptr;
       Turns turns{nullptr, T_all, groups, first, 0, 0, 0};
+      const bool late = status_timed_out(a.status);
       Token cur = load_token(a, first), next{T_all, 0.f, 0}, after = next;
       TokenIn cur_in = load_inputs(a, first), next_in{}, after_in{};
       int ahead = T_all;
@@ -824,6 +835,7 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
       if (!dealt) begin_turns();
       check_token(a, cur, rank == 0);
       cur_in.za = load_target<T>(a, cur);
+      if (late) *abort_flag = 1;  // an earlier call's wait ran out: the inputs may be unwritten
       uint32_t row = 0;
       bool ok = true;
       for (;;) {
@@ -991,7 +1003,12 @@ __global__ void __launch_bounds__(32 * warps_of<Rows, kGrad>(), Rows::kCtas)
   }
   if (C > 1) {
     __syncwarp();
+    if (rank != 0 && lane == 0 && *abort_flag) st_cluster(&abort_flag_s, 0, 1);
     cluster_sync();  // no peer writes here any more (every wait before is bounded)
+    if (rank == 0 && tid == 0 && *abort_flag) {
+      double none[3] = {0.0, 0.0, 0.0};
+      store_sums(none);
+    }
   }
 }
 
@@ -1005,6 +1022,7 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kern
   pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float scale = a.scale;
+  const bool late = threadIdx.x == 0 && status_timed_out(a.status);  // (as in the row kernel)
   double sums[3] = {0.0, 0.0, 0.0};
   const int rows = static_cast<int>(gridDim.x) * kWarps;
   for (int t = static_cast<int>(blockIdx.x) * kWarps + warp; t < a.T; t += rows) {
@@ -1064,6 +1082,7 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kern
     for (int w = 0; w < kWarps; ++w)
 #pragma unroll
       for (int j = 0; j < 3; ++j) s[j] += part[w][j];
+    spoil(s, late);
     if (gridDim.x == 1) {
       write_loss(a, s);
     } else {
