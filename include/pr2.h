@@ -306,7 +306,7 @@ pr2_status pr2_rollout_layers(const pr2_dims* dims, int32_t L, void* h, const vo
  * These calls take any widths (d, m, V odd or even) and, where a row stride is an argument, any
  * stride that holds a row.  Tensors in the layer dtype need the alignment of an element and fp32
  * and int32 ones that of a word; rows that are multiples of 16 bytes apart and start on one run
- * fastest.  dims->T k is at most 2^30. */
+ * fastest.  dims->T k and dims->d are at most 2^30. */
 
 /* Size and constants of one policy-loss call. */
 typedef struct {

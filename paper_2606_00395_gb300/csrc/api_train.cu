@@ -10,6 +10,7 @@ namespace pr2 {
 namespace {
 
 constexpr int64_t kMaxSlots = int64_t{1} << 30;
+constexpr int kMaxWidth = 1 << 30;  // of a token's row: the kernels count columns, a step past it too, in 32 bits
 
 bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) == 0; }
 bool aligned4(std::initializer_list<const void*> ps) {
@@ -43,7 +44,7 @@ pr2_status check_tokens(const pr2_dims* dm) {
   if (dm->dtype != PR2_FP32 && dm->dtype != PR2_BF16) return PR2_ERR_INVALID_ARG;
   if (dm->flags & ~(PR2_F_SYNC_STATUS | PR2_F_DELTA_LOSS | PR2_F_NORMALIZE_TOPK))
     return PR2_ERR_INVALID_ARG;
-  if (dm->N > kMaxExperts || dm->k > kMaxTopKSimt || dm->T > kMaxSlots / dm->k)
+  if (dm->N > kMaxExperts || dm->k > kMaxTopKSimt || dm->T > kMaxSlots / dm->k || dm->d > kMaxWidth)
     return PR2_ERR_UNSUPPORTED;
   return PR2_OK;
 }
