@@ -426,7 +426,8 @@ typedef struct {
  * and for each run of PR2_CKPT_GROUP elements of a row of gate and of up (the last one may be
  * shorter), with top = max |x| over the run:
  *     scale = top / 127,  q = round(x 127 / top)  (to nearest, ties to even; x ~ q scale).
- * The error of a held value is at most half a scale.  A run with top < 1e-30 is held as zeros; a
+ * act is good to about 5e-7 of its size, then rounded once to dtype (the sigmoid's part of that is up to
+ * 4e-6 in bf16).  The error of a held value is at most half a scale.  A run with top < 1e-30 is held as zeros; a
  * run with an infinity or a NaN in it gets the scale NaN, so that its gradient is NaN too.
  *  gate, up [rows, m] with row stride ld; act [rows, m] contiguous;
  *  q [rows, 2, m] int8: a row's gate, then its up; scale [rows, 2, ceil(m / 128)] fp32.
