@@ -7,9 +7,9 @@
 // where the replayed experts have all but vanished; the gates are finite all the same.)
 // 8, 16 or 32 lanes per token, lane s holding slot s, four experts a lane and step: every expert's -rho_j G is
 // stored first, then the selected ones' values over it.  N not a multiple of 4: a warp per token, an expert
-// a lane and step.  Bound by HBM for large batches (rho read, dp written): 262144 x 256 with
-// k = 8 91 us (90 % of the copy rate), 10^6 x 64 with k = 4 117 us (68 %); 4096 x 128 with k = 8
-// is 4.5 MB and takes 4.4 us a call, the host's part.
+// a lane and step.  Bound by HBM for large batches of many experts (rho read, dp written): 262144 x 256 with
+// k = 8 89 us (92 % of the copy rate); 10^6 x 64 with k = 4 113 us (71 %), where a group of lanes has one token's
+// loads in flight; 4096 x 128 with k = 8 is 4.5 MB and takes 3.7 us a call, the host's part.
 #include "pr2_device.cuh"
 #include "pr2_internal.h"
 

@@ -21,11 +21,11 @@
 // second pass frees take the next row's chunks.  The CTAs of a cluster may split a row: they exchange
 // their three sums through distributed shared memory.  Short rows go to one warp each.
 // Bound by HBM (logits read once, gradient written once), and per row by its serial part, some 3 us of
-// joins, exchange and the token's own arithmetic, which the CTAs of an SM overlap; rows of a few KB by what
-// each warp issues per row, so they have CTAs of fewer warps.  Back to back, without
-// masked tokens: 4096 x 131072 bf16 361 us with the gradient (88 % of the copy rate), 161 without (98 %);
-// 8192 x 32001 178 us (87 %); 2048 x 131072 fp32 349 us (91 %); 32768 x 2048 (warps) 72 us (55 %, the
-// token's arithmetic); one token of 131072 7.3 us.
+// joins, exchange and the token's own arithmetic, which the CTAs of an SM overlap.  Rows of a few KB are
+// bound by that part, of which a CTA has one at a time (8192 entries of bf16 with the gradient: HBM 54 %, issue
+// slots 60 %), so they have CTAs of fewer warps.  Back to back, without weights: 4096 x 131072 bf16 364 us
+// with the gradient (87 % of the copy rate), 162 without (98 %); 8192 x 32001 180 us (86 %); 2048 x 131072
+// fp32 349 us (91 %); 32768 x 2048 (warps) 74 us (53 %); one token of 131072 7.2 us.
 // Tokens are dealt to clusters (warps) by their numbers and masks; each sums its tokens' terms in double and
 // policy_finish_kernel the clusters' in order, so the loss does not depend on timing.
 #include <math_constants.h>
@@ -600,13 +600,15 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
 // something, so it is made for long rows in batches of some size only (deals).  us by number / dealt, with none, a
 // tenth, three tenths and half of the tokens masked:
 //   gradient, bf16  4096 x 131072 367/369 361/343 328/305 289/267    8192 x 32001 178/180 175/168 175/148 158/137
-//                   32768 x 16384 369/380 350/351 310/307 296/271    1200 x 32001 39.2/41.2 37.6/40.0 35.5/35.1 32.7/32.2
+//                   32768 x 16384 369/380 350/351 310/307 296/271
+//                   1200 x 32001 39.2/41.2 37.6/40.0 35.5/35.1 32.7/32.2
 //                   8192 x 8192 60.9/64.5 60.0/60.5 56.2/53.0 51.1/45.9   65536 x 16384 727/748 691/695 607/607 561/538
 //   forward, bf16   4096 x 131072 163/168 156/150 138/120 114/91     8192 x 50001 134/138 131/126 123/103 100/79
 //                   1500 x 131072 66.5/71.3 64.2/65.5 61.3/53.3 55.7/45.7
 //                   2048 x 65000 49.1/54.0 48.2/50.1 45.0/43.3 41.6/35.5
 //                   16384 x 16384 100/107 96/99 86/83 71/69    65536 x 32000 654/675 612/615 507/499 393/381
-//   forward, fp32   8192 x 32768 162/166 149/152 123/122 91/93       2400 x 32001 53.6/58.2 50.1/53.4 42.1/44.0 35.8/34.7
+//   forward, fp32   8192 x 32768 162/166 149/152 123/122 91/93
+//                   2400 x 32001 53.6/58.2 50.1/53.4 42.1/44.0 35.8/34.7
 constexpr int kDealThreads = 1024, kDealVecs = 8;
 
 __global__ void __launch_bounds__(kDealThreads) policy_deal_kernel(const float* weight, int T, int groups,
@@ -1050,7 +1052,7 @@ __global__ void __launch_bounds__(kThreads, kHeld <= 8 ? 3 : 2) policy_warp_kern
       if (edge >= 0) ez = to_f32<T>(row[edge]);
 #pragma unroll
       for (int j = 0; j < kHeld; j += kVecs)
-        if (j * 32 < sh.nvec) 
+        if (j * 32 < sh.nvec)
           add_vectors<T>(s, M, reinterpret_cast<const uint4(&)[kVecs]>(raw[j]), src, j * 32 + lane, 32, sh.nvec, scale);
       if (edge >= 0) add_one(s, ez, scale);
       s = join_lanes<32>(s, scale);

@@ -772,9 +772,17 @@ cudaError_t sum_rows(const TokenArgs& a, int num_sms, cudaStream_t st) {
 }
 
 // unsort_backward: a block a token for few tokens, and for tokens of much work (eight pieces of a row for
-// each warp) while a warp a token would leave the SMs unevenly filled; else a warp a token (bf16, k = 8, us
-// with a warp / a block: 4096 x 2048 60.2 / 47.3, 8192 x 7168 341 / 321, 32768 x 2048 351 / 374, 4096 x 512
-// 14.0 / 26.1).
+// each warp) while a warp a token would leave the SMs unevenly filled; else a warp a token.  us with a warp / a
+// block, "=" where the rule takes the slower one:
+//   bf16, k = 8  2048 columns 4096 60.1 / 47.3, 9728 (the switch) 111 / 112, 12000 139 / 136 =, 32768 352 / 374;
+//                7168 columns 8192 340 / 320, 9728 372 / 382, 12000 474 / 465 =, 32768 1219 / 1274;
+//                512 columns 4096 14.0 / 26.1; 2047 columns 1000 38 / 18, 8192 154 / 159 =, 9728 170 / 187
+//   bf16, k = 2  2048 columns 200 8.4 / 4.6, 304 (the switch) 8.3 / 4.5 =, 1000 8.4 / 6.8 =, 8192 40 / 45;
+//                7168 columns 1000 32 / 17 =, 4096 81 / 64 =, 9728 136 / 154
+//   fp32, k = 8  4096 columns 4096 208 / 169, 9728 409 / 408, 16384 685 / 681;
+//                1023 columns 1000 26.6 / 13.8, 4096 69 / 76 =, 9728 155 / 170
+//   fp32, k = 2  4096 columns 8192 139 / 113, 9728 148 / 132 =, 32768 463 / 434 =; 1024 columns 1000 8.8 / 5.7 =,
+//                9728 41 / 44
 template <typename T>
 cudaError_t launch_unsort_backward(void (*warps)(const T*, const T*, const float*, const int32_t*, const int32_t*, int,
                                                  int, int, int, T*, float*),
