@@ -344,6 +344,7 @@ typedef struct {
  *  An entry of -inf is a token that cannot be sampled: p = 0, gradient 0.  A row of nothing but
  *  -inf has no distribution: it contributes nothing, its logp is -inf, its entropy and gradient 0.
  *  A target outside [0, V) sets PR2_STATUS_BAD_INDEX and counts as a token of weight 0.
+ *  logp is at most 0 and entropy at least 0.
  *  T = 0 writes loss 0.  fp32 arithmetic, the gradient rounded once.  Deterministic.
  *  A bounded wait that runs out, in this call or (PR2_STATUS_TIMEOUT in status_dev) before it, makes
  *  loss NaN, with or without a status word; the other outputs are unspecified then.
