@@ -314,8 +314,6 @@ struct alignas(32) Job {
   int unused;
 };
 
-__device__ __forceinline__ int round32(int n) { return (n + 31) & ~31; }
-
 template <int kOp, typename L>
 struct Plan {
   static constexpr int kBlock = L::kBlock;
@@ -329,8 +327,8 @@ struct Plan {
   __device__ __forceinline__ static int tiles_of(int n) {
     return L::kTileRows > L::kCols && n > 0 && n <= L::kTileRows ? 1 : (n + L::kCols - 1) / L::kCols;
   }
-  // Job j, false if there is nothing to do; at is where to look from (j ascends).  A whole warp calls it.
-  __device__ __forceinline__ bool job(const GroupArgs& g, int j, int& at, Job& b) const {
+  // Job j, false if there is nothing to do.  A whole warp calls it.
+  __device__ __forceinline__ bool job(const GroupArgs& g, int j, Job& b) const {
     b = Job{};
     if (j >= total) return false;
     if constexpr (kOp == kGroupWeight) {
@@ -347,25 +345,14 @@ struct Plan {
       return b.kb > 0 || !g.accumulate;
     } else {
       const int lane = threadIdx.x & 31;
-      for (;;) {
-        const uint32_t past = __ballot_sync(0xffffffffu, at + lane < g.N && j < prefix[at + lane + 1]);
-        if (past != 0u) {
-          at += __ffs(past) - 1;
-          break;
-        }
-        at += 32;
-        if (at >= g.N) return false;  // (not with j < total)
-      }
-      b.e = at;
+      auto lowest = [&](auto holds) { return __ffs(__ballot_sync(0xffffffffu, holds(lane))) - 1; };
+      b.e = expert_of_job(prefix, g.N, j, lowest);
       const ExpertRows all = expert_rows(g.offsets, b.e, static_cast<int>(g.rows));
       const int n = all.hi - all.lo;
-      const int tiles = tiles_of(n);
-      const int size = round32((n + tiles - 1) / tiles);  // rows of this expert's tiles
-      const int i = j - prefix[at];
-      const int r = i % tiles * size;
-      b.m0 = i / tiles * (kOp == kGroupForward && g.pairs == 2 ? 128 : 256);
-      b.row0 = all.lo + r;
-      b.rows = n - r < size ? n - r : size;
+      const RowTile t = row_tile(all.lo, n, tiles_of(n), j - prefix[b.e]);
+      b.m0 = t.block * (kOp == kGroupForward && g.pairs == 2 ? 128 : 256);
+      b.row0 = t.row0;
+      b.rows = t.rows;
       b.kb = kOp == kGroupForward ? (g.d_in + kBlock - 1) / kBlock : g.pairs * ((g.d_out + kBlock - 1) / kBlock);
       return b.rows > 0;
     }
@@ -1187,9 +1174,9 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   } else if (warp == kSchedWarp) {
     // ---------------- scheduler ----------------
     const uint32_t answer_there = mapa_shared(smem_u32(answer), 1), heard_at = mapa_shared(smem_u32(heard), 0);
-    int j = static_cast<int>(blockIdx.x >> 1), at = 0, n = 0, asked = 0;
+    int j = static_cast<int>(blockIdx.x >> 1), n = 0, asked = 0;
     for (;;) {
-      const bool work = plan.job(g, j, at, b);
+      const bool work = plan.job(g, j, b);
       bool more = true;
       if (work) {
         const int slot = n % kJobs;
