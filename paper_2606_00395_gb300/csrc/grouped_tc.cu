@@ -1385,10 +1385,14 @@ bool on16(const void* p, int64_t row_bytes) {
 template <int kOp, int kType, typename TC, int kLoaders>
 cudaError_t launch_pairs(const TcMaps& m, const GroupArgs& g, const TcFlags& fl, int pairs, cudaStream_t st) {
   auto* kernel = grouped_tc_kernel<kOp, kType, TC, kLoaders>;
-  const int smem = Layout<kOp, kType, kLoaders>::kBytes + kPlanBytes * ((g.N + 3) & ~3);
+  constexpr int kBytes = Layout<kOp, kType, kLoaders>::kBytes;
+  const int smem = kBytes + kPlanBytes * ((g.N + 3) & ~3);
   using R = Roles<kOp, kType, kLoaders>;
   static_assert(!R::kKeep || R::kThreads == kKeepThreads, "threads");
-  cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // The limit is the kernel's, not the launch's: the same for every number of experts, so that a call with fewer
+  // of them on another host thread cannot lower it between this and a launch.
+  cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         kBytes + kPlanBytes * kMaxExpertsDispatch);
   if (err != cudaSuccess) return err;
   if constexpr (R::kKeep) {  // without the registers that the epilogue takes over it would wait forever
     static const int regs = [kernel] {
