@@ -21,7 +21,7 @@
 // The tensor core adds to its fp32 accumulator by cutting bits off, so the error of a long sum grows with
 // its length and to one side (8192 rows: 9e-6 of the norm, 512: 5e-7; fp32 FMAs in turn 3e-7).  Results in
 // fp32 therefore leave the accumulator every kMostMmas MMAs and are added up, rounded, where they are stored, by the
-// thread or the copies of the warp that stored them before.
+// thread or the copies of the warp that stored them before; results in 16 bits every kLongMmas, in tensor memory.
 //
 // fp32 operands: each value is a sum of three bf16 values (24 bits), and six of the nine products of their
 // planes, the first in an accumulator of its own, give the fp32 product to 2^-24 (see split3).
@@ -75,6 +75,11 @@ constexpr int kRawPitch = 144;                  // 128 bytes from anywhere in a 
 // MMAs in turn that a result in fp32 takes from one accumulator: of 16-bit operands 48 (relative error 7e-7; 32: 5e-7 and
 // an eighth more time for gradients of matrices of many rows), of fp32 ones 32; 16 where registers keep the sums.
 constexpr int kMostMmas = 48, kExactMmas = 32, kKeepMmas = 16;
+// And that a result in 16 bits takes (16384 bf16 or 32768 e4m3 columns): 8e-5 of a sum of terms of one sign, 4 % of half
+// a step.  Longer sums (to one side 8e-4 at 131072 columns, 7e-3 at 2^20, where no value was rounded right) use one
+// accumulator and add it every so many MMAs to their sums in the other, whose epilogue then overlaps nothing (8192
+// rows, 8 matrices of 2048 x 32768: 666 us, as before; every 512 MMAs, 3e-5: 689).
+constexpr int kLongMmas = 1024;
 
 constexpr int kPlanBytes = 4;  // an expert: place in the order, or jobs before it
 
@@ -302,6 +307,35 @@ __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uin
   }
 }
 
+// 16 columns of this lane into tensor memory, there for later loads of this warp after tmem_wait_st().
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A warp's columns of an accumulator (16 of every 32, from c0 on) to, or onto, the sums.  Out of the way of the
+// epilogue's registers.
+static __device__ __noinline__ void add_chunk(uint32_t tacc, uint32_t tsum, int c0, int cols, bool add) {
+  for (; c0 < cols; c0 += 32) {
+    uint32_t v[16], sum[16];
+    tmem_ld16(tacc + c0, v);
+    if (add) tmem_ld16(tsum + c0, sum);
+    tmem_wait_ld(v);
+    if (add) {
+      reg_fence(sum);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(sum[j]));
+    }
+    tmem_st16(tsum + c0, v);
+  }
+  tmem_wait_st();
+}
+
 // ---- jobs -------------------------------------------------------------------------------------
 struct alignas(32) Job {
   int e;     // expert; -1: no more jobs
@@ -318,14 +352,16 @@ template <int kOp, typename L>
 struct Plan {
   static constexpr int kBlock = L::kBlock;
   int total, m_blocks, n_blocks, each;  // each: jobs of an expert (weight)
+  int kb;       // forward, rows: K blocks of every job
+  bool longer;  // forward, rows: more of them than an accumulator takes in turn (kLongBlocks)
   int* order;   // [N], in shared memory; weight: experts, those of most rows and of fewest in turn
   int* prefix;  // [N + 1] forward, rows: jobs of the experts before
   // Tiles of n rows.  Up to 384 rows are one tile although it fills both accumulators, so that no epilogue
   // overlaps the next tile's MMAs: an expert's matrices then leave L2 once (128 experts of 256 rows in the mean:
   // forward 196 -> 180 us).  More rows go in tiles of at most 256 (e4m3, 128 experts of 1024 rows in the mean: 300 us;
   // of 288 where that makes one less 316, of 384 344).
-  __device__ __forceinline__ static int tiles_of(int n) {
-    return L::kTileRows > L::kCols && n > 0 && n <= L::kTileRows ? 1 : (n + L::kCols - 1) / L::kCols;
+  __device__ __forceinline__ int tiles_of(int n) const {
+    return L::kTileRows > L::kCols && !longer && n > 0 && n <= L::kTileRows ? 1 : (n + L::kCols - 1) / L::kCols;
   }
   // Job j, false if there is nothing to do.  A whole warp calls it.
   __device__ __forceinline__ bool job(const GroupArgs& g, int j, Job& b) const {
@@ -353,7 +389,7 @@ struct Plan {
       b.m0 = t.block * (kOp == kGroupForward && g.pairs == 2 ? 128 : 256);
       b.row0 = t.row0;
       b.rows = t.rows;
-      b.kb = kOp == kGroupForward ? (g.d_in + kBlock - 1) / kBlock : g.pairs * ((g.d_out + kBlock - 1) / kBlock);
+      b.kb = kb;
       return b.rows > 0;
     }
   }
@@ -583,6 +619,9 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   constexpr int kEpiWarp0 = R::kEpi0, kSchedWarp = R::kSched, kLoadWarp0 = R::kLoad0;
   constexpr int kMmas = kType == kE4m3 ? 4 : kBlock / 16;  // of a K block, in turn
   constexpr int kChunk = sizeof(TC) == 2 ? 1 << 30 : (R::kKeep ? kKeepMmas : kSplit ? kExactMmas : kMostMmas) / kMmas;
+  // Results in 16 bits: longer sums leave the accumulator too, for its neighbour (see kLongMmas)
+  constexpr bool kLong = sizeof(TC) == 2 && kOp != kGroupWeight;
+  constexpr int kLongBlocks = kLongMmas / kMmas;
   constexpr bool kAMn = kOp != kGroupForward, kBMn = kOp == kGroupWeight;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -667,6 +706,8 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
       }
       __syncthreads();
     }
+    plan.kb = kOp == kGroupForward ? (g.d_in + kBlock - 1) / kBlock : g.pairs * ((g.d_out + kBlock - 1) / kBlock);
+    plan.longer = kLong && plan.kb > kLongBlocks;
     plan.n_blocks = kOp == kGroupWeight ? (g.d_in + L::kCols - 1) / L::kCols : (g.d_in + 255) / 256;
     if constexpr (kOp == kGroupWeight) {
       plan.m_blocks = (g.d_out + 255) / 256;
@@ -678,7 +719,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
       if (warp == 0) {
         const int per = (N + 31) / 32, e0 = lane * per, e1 = e0 + per < N ? e0 + per : N;  // a lane's experts
         int own = 0;
-        for (int e = e0; e < e1; ++e) own += Plan<kOp, L>::tiles_of(cnt[e]) * plan.m_blocks;
+        for (int e = e0; e < e1; ++e) own += plan.tiles_of(cnt[e]) * plan.m_blocks;
         int upto = own;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -687,7 +728,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         }
         upto -= own;
         for (int e = e0; e < e1; ++e) {
-          upto += Plan<kOp, L>::tiles_of(cnt[e]) * plan.m_blocks;
+          upto += plan.tiles_of(cnt[e]) * plan.m_blocks;
           plan.prefix[e + 1] = upto;
         }
         if (lane == 0) plan.prefix[0] = 0;
@@ -702,6 +743,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   auto columns = [&](const Job& b) {
     return kOp == kGroupWeight ? (L::kCols == 128 || g.d_in - b.n0 <= 128 ? 128 : 256) : round32(b.rows);
   };
+  auto longer = [](const Job& b) { return kLong && b.kb > kLongBlocks; };
   // rows of a tile's first accumulator: all, or half of more than one holds
   auto first_rows = [&](const Job& b) {
     return kOp == kGroupWeight || b.rows <= L::kCols ? b.rows : round32((b.rows + 1) / 2);
@@ -828,7 +870,9 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
       }
       // each chunk of K (results in fp32), and of each the one or two accumulators of the tile's rows
       const int rows0 = first_rows(b), rows_all = b.rows, row_first = b.row0;
-      const int parts = rows0 < rows_all ? 2 : 1, sums = b.kb <= kChunk ? 1 : (b.kb + kChunk - 1) / kChunk;
+      // (a longer sum has both accumulators, of which the second takes no MMAs: it holds the chunks' sums)
+      const int parts = rows0 < rows_all || longer(b) ? 2 : 1;
+      const int per = longer(b) ? kLongBlocks : kChunk, sums = b.kb <= per ? 1 : (b.kb + per - 1) / per;
       for (int i = 0; i < parts * sums && in; ++i) {
         const int chunk = i / parts;
         if (parts == 2) {
@@ -836,7 +880,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
           b.row0 = row_first + (i % 2 == 0 ? 0 : rows0);
         }
         const int buf = used & 1;
-        const uint32_t tacc = tq + buf * kAccCols;
+        uint32_t tacc = tq + buf * kAccCols;
         auto wait_acc = [&]() { return b.kb == 0 || wait_pair<kHere, R::kKeep>(&acc_full[buf], (used >> 1) & 1, abort_flag, g.status); };
         if constexpr (kOp == kGroupWeight) {
           in = wait_acc();
@@ -875,12 +919,22 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
             row_scale = r < b.rows ? g.scale[b.row0 + r] : 0.f;
           }
           in = wait_acc();
+          auto add_sums = [&]() {  // the results stand in the other accumulator then, once all chunks have been added
+            if constexpr (kLong) {
+              if (!longer(b) || i % 2 != 0) return;
+              const uint32_t tsum = tq + (buf ^ 1) * kAccCols;
+              add_chunk(tacc, tsum, side * 16, b.rows, chunk > 0);
+              tacc = tsum;
+              if (chunk + 1 < sums) b.rows = 0;  // nothing to store yet
+            }
+          };
           if (sizeof(TC) == 2 && fl.vec_out) {
             // fragments with the rows along registers, transposed by stmatrix into a [16][128] buffer of the
             // side, stored as 256 contiguous bytes a row
             in = named_bar_and(1 + side, 128, in);
             if (!in) break;
             tc_fence_after();
+            add_sums();
             const int st_id = ((warp - kEpiWarp0) & 3) * 32 + lane;
             const uint32_t obuf = smem_u32(smem + L::kOut + side * 2 * kOutBuf);
             const uint32_t ost = static_cast<uint32_t>((lane & 7) * kOutPitch + q * 64 + (lane >> 3) * 16);
@@ -937,6 +991,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
             // a row's 32 neighbouring columns are a warp's lanes: single elements, 32 in a run
             if (!in) break;
             tc_fence_after();
+            add_sums();
             const int o = 32 * q + lane;
             const bool live = c128 + o < width;
             const float own = k8 && live ? wscale[c128 + o] : 0.f;
@@ -1086,18 +1141,19 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         const int rows0 = first_rows(b), rows1 = b.rows - rows0;
         const int cols0 = kOp == kGroupWeight ? columns(b) : round32(rows0);
         const bool two = L::kTileRows > L::kCols && kOp != kGroupWeight && rows1 > 0;
+        const bool both = two || longer(b);
         const uint32_t idesc = kIdesc | (static_cast<uint32_t>(cols0) >> 3 << 17);
         const uint32_t idesc1 = kIdesc | (static_cast<uint32_t>(round32(rows1)) >> 3 << 17);
         uint32_t d = 0;
         for (int kb = 0; kb < b.kb; ++kb) {
-          const bool first = kb % kChunk == 0;
+          const bool first = longer(b) ? kb % kLongBlocks == 0 : kb % kChunk == 0;
           if (first) {
             const int buf = used & 1;
             if (!wait_pair<kAnywhere, R::kKeep>(&acc_empty[buf], ((used >> 1) & 1) ^ 1, abort_flag, g.status)) {
               ok = false;
               break;
             }
-            if (two && !wait_pair<kAnywhere, R::kKeep>(&acc_empty[buf ^ 1], (((used + 1) >> 1) & 1) ^ 1, abort_flag, g.status)) {
+            if (both && !wait_pair<kAnywhere, R::kKeep>(&acc_empty[buf ^ 1], (((used + 1) >> 1) & 1) ^ 1, abort_flag, g.status)) {
               ok = false;
               break;
             }
@@ -1127,7 +1183,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
               }
             }
           }
-          const bool last = kb + 1 == b.kb || (kb + 1) % kChunk == 0;
+          const bool last = kb + 1 == b.kb || (longer(b) ? (kb + 1) % kLongBlocks == 0 : (kb + 1) % kChunk == 0);
           if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < kMmas; ++kk) {
@@ -1147,6 +1203,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
               }
             }
             if (last) pair_commit(&acc_full[used & 1]);
+            if (longer(b) && last) pair_commit(&acc_full[(used & 1) ^ 1]);
             if (two) {  // the tile's other rows, against the same A
               const uint32_t lb1 = lb + cols0 / 2 * (128 / 16), d1 = tm + ((used & 1) ^ 1) * kAccCols;
 #pragma unroll
@@ -1158,7 +1215,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
             pair_commit(&empty[stage]);
           }
           __syncwarp();
-          if (last) used += two ? 2 : 1;
+          if (last) used += both ? 2 : 1;
           if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
