@@ -1427,6 +1427,13 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   }
   if (kOp == kGroupWeight && fl.vec_out && epilogue && lane == 0) bulk_wait_all();
   __syncthreads();
+  // Once a role has given up, copies and launch control's answer may be in flight that nobody waits for: this CTA
+  // stays until they have long landed.  (Without that each has been waited for where it was used.)
+  if (*abort_flag) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < kDrainLimitNs) __nanosleep(1000);
+    __syncthreads();
+  }
   cluster_sync();  // neither CTA leaves while the other may still reach it
   if (warp == kWarpMma) {
     tc_fence_after();
