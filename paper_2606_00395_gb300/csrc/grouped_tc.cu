@@ -177,11 +177,12 @@ static __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, vo
 // A whole warp waits; true if every lane saw the phase complete.  kInline: without a call, across which few
 // registers could be kept.
 template <int kFrom, bool kInline>
-__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+__device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int32_t* status,
+                                          uint64_t limit_ns = kWaitLimitNs) {
   bool in = try_wait_pair<kFrom>(bar, parity);
   if (!in) {
-    in = kInline ? wait_until<kFrom>(bar, parity, abort_flag, status, kWaitLimitNs)
-                 : wait_slow<kFrom>(bar, parity, abort_flag, status, kWaitLimitNs);
+    in = kInline ? wait_until<kFrom>(bar, parity, abort_flag, status, limit_ns)
+                 : wait_slow<kFrom>(bar, parity, abort_flag, status, limit_ns);
   }
   return __all_sync(0xffffffffu, in);
 }
@@ -395,15 +396,31 @@ struct Plan {
   }
 };
 
+// Waits that last as long as jobs do (all others wait for a step of the pipeline): for the loads of a job to come to
+// their end, and what follows from that.  A job walks all rows of an expert, up to 2^30, so they run out after the usual
+// limit and 20 us for each K block of the jobs that may be under way (one takes 0.3 to 1.6 us).
+constexpr uint64_t kBlockLimitNs = 20000;
+struct UnderWay {
+  int64_t last = 0, before = 0;  // K blocks of the job before and of the one before that
+  // The limit while a job of kb blocks and those two are under way; it is the last one then.
+  __device__ __forceinline__ uint64_t limit(int kb) {
+    const uint64_t blocks = static_cast<uint64_t>(kb + last + before);
+    before = last;
+    last = kb;
+    return kWaitLimitNs + blocks * kBlockLimitNs;
+  }
+};
+
 // A role's way through the scheduler's jobs: every warp of it reads each one and lets its place go.
 struct JobReader {
   const Job* ring;
   uint64_t *full, *empty;
   int n = 0;
   template <bool kInline>
-  __device__ __forceinline__ bool next(Job& b, volatile int* abort_flag, int32_t* status) {
+  __device__ __forceinline__ bool next(Job& b, volatile int* abort_flag, int32_t* status,
+                                       uint64_t limit_ns = kWaitLimitNs) {
     const int slot = n % kJobs;
-    if (!wait_pair<kHere, kInline>(&full[slot], (n / kJobs) & 1, abort_flag, status)) return false;
+    if (!wait_pair<kHere, kInline>(&full[slot], (n / kJobs) & 1, abort_flag, status, limit_ns)) return false;
     ++n;
     const int4* p = reinterpret_cast<const int4*>(&ring[slot]);
     const int4 u = p[0], v = p[1];
@@ -1232,10 +1249,13 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
     // ---------------- scheduler ----------------
     const uint32_t answer_there = mapa_shared(smem_u32(answer), 1), heard_at = mapa_shared(smem_u32(heard), 0);
     int j = static_cast<int>(blockIdx.x >> 1), n = 0, asked = 0;
+    UnderWay jobs_under_way;
+    uint64_t limit = kWaitLimitNs;
     for (;;) {
       const bool work = plan.job(g, j, b);
       bool more = true;
       if (work) {
+        limit = jobs_under_way.limit(b.kb);
         const int slot = n % kJobs;
         if (n >= kJobs && !wait_pair<kHere, R::kKeep>(&job_empty[slot], ((n / kJobs) & 1) ^ 1, abort_flag, g.status)) break;
         if (lane == 0) {
@@ -1249,7 +1269,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         // The next job is taken when the loads of this one are nearly issued, not sooner: others may be free
         // before.  Behind a short one (an answer takes about 1.4 us) two are kept in hand.
         const int of = b.kb > kAskAhead ? n - 1 : n - 2;
-        if (rank == 0 && of >= 0) more = wait_pair<kHere, R::kKeep>(&want[of & 1], (of >> 1) & 1, abort_flag, g.status);
+        if (rank == 0 && of >= 0) more = wait_pair<kHere, R::kKeep>(&want[of & 1], (of >> 1) & 1, abort_flag, g.status, limit);
       }
       if (rank == 0) {
         if (asked > 0) more = wait_pair<kAnywhere, R::kKeep>(heard, (asked - 1) & 1, abort_flag, g.status) && more;
@@ -1261,7 +1281,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         }
         __syncwarp();
       }
-      if (!wait_pair<kHere, R::kKeep>(answer, asked & 1, abort_flag, g.status)) break;
+      if (!wait_pair<kHere, R::kKeep>(answer, asked & 1, abort_flag, g.status, limit)) break;
       ++asked;
       uint32_t cta;
       more = taken(smem_u32(response), cta);
@@ -1286,12 +1306,15 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
     const uint32_t done = mapa_shared(smem_u32(zeroed), 0);
     uint32_t tail_phase = 0;  // a bit for each stage
     int64_t blocks = 0;       // K blocks before this job
-    while (jobs.next<R::kKeep>(b, abort_flag, g.status)) {
+    UnderWay jobs_under_way;
+    uint64_t limit = kWaitLimitNs;
+    while (jobs.next<R::kKeep>(b, abort_flag, g.status, limit)) {
       blocks += b.kb;
+      limit = jobs_under_way.limit(b.kb);
       const int left = b.rows % kBlock;
       if (left == 0) continue;
       const int stage = static_cast<int>((blocks - 1) % kStages);
-      if (!wait_pair<kHere, R::kKeep>(&tail[stage], (tail_phase >> stage) & 1u, abort_flag, g.status)) break;
+      if (!wait_pair<kHere, R::kKeep>(&tail[stage], (tail_phase >> stage) & 1u, abort_flag, g.status, limit)) break;
       tail_phase ^= 1u << stage;
       zero_rows(sbase + stage * kStage, left, 15, w, kLoadWarps<kLoaders>);
       release_shared();
