@@ -537,12 +537,12 @@ struct RawRows {
 };
 
 // x = hi + mid + lo, each bf16, to the last bit of fp32: hi is x cut off after 8 bits (which cannot overflow and
-// keeps infinities; what an infinity or a NaN leaves is NaN), mid the rest to nearest, lo what that leaves, of
-// either sign.  |mid| is below 2^-7 of x and |lo| below 2^-16, so the products left out (mid lo, lo mid, lo lo)
+// keeps infinities and, unlike its upper half word, any NaN), mid the rest to nearest, lo what that leaves, of
+// either sign.  An infinity leaves NaN there, but hi's products alone say what it comes to: see the epilogue.  |mid| is below 2^-7 of x and |lo| below 2^-16, so the products left out (mid lo, lo mid, lo lo)
 // are below 2^-22 of a product, about 2^-25 in the mean.  Two values at once, in the halves of a word a plane.
 __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
   const uint32_t bx = __float_as_uint(x), by = __float_as_uint(y);
-  hi = __byte_perm(bx, by, 0x7632);
+  asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
   const float rx = x - __uint_as_float(bx & 0xffff0000u), ry = y - __uint_as_float(by & 0xffff0000u);
   mid = pack_bf16x2(rx, ry);
   lo = pack_bf16x2(rx - __uint_as_float(mid << 16), ry - __uint_as_float(mid & 0xffff0000u));
@@ -793,7 +793,10 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
       if constexpr (kSplit) {
         reg_fence(small);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(small[i]));
+        for (int i = 0; i < 16; ++i) {  // (beside an infinity the small products are whatever its planes gave)
+          const float large = __uint_as_float(v[i]);
+          if (fabsf(large) < INFINITY) v[i] = __float_as_uint(large + __uint_as_float(small[i]));
+        }
       }
     };
     // Gradient of the matrices: 32 x 16 blocks through two buffers of the warp (64-byte swizzle: the 16-byte
