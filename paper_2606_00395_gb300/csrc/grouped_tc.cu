@@ -23,8 +23,8 @@
 // fp32 therefore leave the accumulator every kMostMmas MMAs and are added up, rounded, where they are stored, by the
 // thread or the copies of the warp that stored them before; results in 16 bits every kLongMmas, in tensor memory.
 //
-// fp32 operands: each value is a sum of three bf16 values (24 bits), and six of the nine products of their
-// planes, the first in an accumulator of its own, give the fp32 product to 2^-24 (see split3).
+// fp32 operands: each value is a sum of three bf16 values (24 bits), and eight of the nine products of their
+// planes, the first in an accumulator of its own, give the product to 2^-32 (see split3).
 //
 // The launch has a pair for every job.  A pair that runs takes further jobs over from pairs that have not
 // started (cluster launch control), so that the pairs end at about the same time whatever the experts'
@@ -538,8 +538,10 @@ struct RawRows {
 
 // x = hi + mid + lo, each bf16, to the last bit of fp32: hi is x cut off after 8 bits (which cannot overflow and
 // keeps infinities and, unlike its upper half word, any NaN), mid the rest to nearest, lo what that leaves, of
-// either sign.  An infinity leaves NaN there, but hi's products alone say what it comes to: see the epilogue.  |mid| is below 2^-7 of x and |lo| below 2^-16, so the products left out (mid lo, lo mid, lo lo)
-// are below 2^-22 of a product, about 2^-25 in the mean.  Two values at once, in the halves of a word a plane.
+// either sign.  |mid| is below 2^-7 of x and |lo| below 2^-16, so the product left out (lo lo) is below 2^-32 of a
+// product.  (Without mid lo and lo mid too it was 2^-22, and a K block took as long: the loaders bound it.)  An infinity
+// leaves NaN in mid, but hi's products alone say what it comes to: see the epilogue.  Two values at once, in the
+// halves of a word a plane.
 __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
   const uint32_t bx = __float_as_uint(x), by = __float_as_uint(y);
   asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
@@ -1215,7 +1217,9 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
               };
               mma(d, 0, 0, more);
               if constexpr (kSplit) {  // the small products apart: they are added to the large ones at the end
-                mma(d + kAccCols / 2, 0, 2, more);
+                mma(d + kAccCols / 2, 1, 2, more);
+                mma(d + kAccCols / 2, 2, 1, 1u);
+                mma(d + kAccCols / 2, 0, 2, 1u);
                 mma(d + kAccCols / 2, 2, 0, 1u);
                 mma(d + kAccCols / 2, 1, 1, 1u);
                 mma(d + kAccCols / 2, 0, 1, 1u);
