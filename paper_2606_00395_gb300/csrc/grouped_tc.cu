@@ -81,6 +81,9 @@ constexpr int kMostMmas = 48, kExactMmas = 32, kKeepMmas = 16;
 // rows, 8 matrices of 2048 x 32768: 666 us, as before; every 512 MMAs, 3e-5: 689).
 constexpr int kLongMmas = 1024;
 
+// e4m3: K blocks (4096 columns) from which on up to 384 rows of an expert are one tile (see Plan)
+constexpr int kWideBlocks = 32;
+
 constexpr int kPlanBytes = 4;  // an expert: place in the order, or jobs before it
 
 template <int kOp, int kType, int kLoaders>
@@ -353,16 +356,19 @@ template <int kOp, typename L>
 struct Plan {
   static constexpr int kBlock = L::kBlock;
   int total, m_blocks, n_blocks, each;  // each: jobs of an expert (weight)
-  int kb;       // forward, rows: K blocks of every job
-  bool longer;  // forward, rows: more of them than an accumulator takes in turn (kLongBlocks)
+  int kb;    // forward, rows: K blocks of every job
+  int most;  // forward, rows: of an expert's rows that are one tile whatever kCols is
   int* order;   // [N], in shared memory; weight: experts, those of most rows and of fewest in turn
   int* prefix;  // [N + 1] forward, rows: jobs of the experts before
   // Tiles of n rows.  Up to 384 rows are one tile although it fills both accumulators, so that no epilogue
-  // overlaps the next tile's MMAs: an expert's matrices then leave L2 once (128 experts of 256 rows in the mean:
-  // forward 196 -> 180 us).  More rows go in tiles of at most 256 (e4m3, 128 experts of 1024 rows in the mean: 300 us;
-  // of 288 where that makes one less 316, of 384 344).
+  // overlaps the next tile's MMAs: an expert's matrices then leave L2 once (128 experts of 320 rows, bf16, 2048 to 2 x
+  // 768 columns: 197 us, in tiles of at most 256 rows 234; 512 to 2048 columns 95, 103).  More rows go in tiles of at
+  // most 256 (bf16, 128 experts of 256 rows in the mean, 384 for all: 242 us against 238).  e4m3, whose K blocks of 128
+  // columns cost as much, so that the epilogue weighs more, only from 4096 columns on (320 rows: 7168 to 2 x 2048 226 us
+  // against 259 in tiles of 256, 4096 to 2 x 1024 156, 165; 3584 142, 146 and to 1024 93, 87; 2048 to 2 x 768 148, 134;
+  // 768 to 2048 117, 97).
   __device__ __forceinline__ int tiles_of(int n) const {
-    return L::kTileRows > L::kCols && !longer && n > 0 && n <= L::kTileRows ? 1 : (n + L::kCols - 1) / L::kCols;
+    return L::kTileRows > L::kCols && n > 0 && n <= most ? 1 : (n + L::kCols - 1) / L::kCols;
   }
   // Job j, false if there is nothing to do.  A whole warp calls it.
   __device__ __forceinline__ bool job(const GroupArgs& g, int j, Job& b) const {
@@ -539,9 +545,10 @@ struct RawRows {
 // x = hi + mid + lo, each bf16, to the last bit of fp32: hi is x cut off after 8 bits (which cannot overflow and
 // keeps infinities and, unlike its upper half word, any NaN), mid the rest to nearest, lo what that leaves, of
 // either sign.  |mid| is below 2^-7 of x and |lo| below 2^-16, so the product left out (lo lo) is below 2^-32 of a
-// product.  (Without mid lo and lo mid too it was 2^-22, and a K block took as long: the loaders bound it.)  An infinity
-// leaves NaN in mid, but hi's products alone say what it comes to: see the epilogue.  Two values at once, in the
-// halves of a word a plane.
+// product.  (Without mid lo and lo mid it is 2^-22, four units, for 1 to 4 % less time: 1001 tokens, 16 experts of
+// 1000 x 515 51.6 us against 52.1, both gradients of 517 tokens, 60 experts of 192 x 250 35.2 against 36.7.)  An
+// infinity leaves NaN in mid, but hi's products alone say what it comes to: see the epilogue.  Two values at once, in
+// the halves of a word a plane.
 __device__ __forceinline__ void split3(float x, float y, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
   const uint32_t bx = __float_as_uint(x), by = __float_as_uint(y);
   asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
@@ -641,6 +648,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   // Results in 16 bits: longer sums leave the accumulator too, for its neighbour (see kLongMmas)
   constexpr bool kLong = sizeof(TC) == 2 && kOp != kGroupWeight;
   constexpr int kLongBlocks = kLongMmas / kMmas;
+  static_assert((kLongBlocks & (kLongBlocks - 1)) == 0, "power of two");
   constexpr bool kAMn = kOp != kGroupForward, kBMn = kOp == kGroupWeight;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -726,7 +734,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
       __syncthreads();
     }
     plan.kb = kOp == kGroupForward ? (g.d_in + kBlock - 1) / kBlock : g.pairs * ((g.d_out + kBlock - 1) / kBlock);
-    plan.longer = kLong && plan.kb > kLongBlocks;
+    plan.most = (kLong && plan.kb > kLongBlocks) || (k8 && plan.kb < kWideBlocks) ? 0 : L::kTileRows;
     plan.n_blocks = kOp == kGroupWeight ? (g.d_in + L::kCols - 1) / L::kCols : (g.d_in + 255) / 256;
     if constexpr (kOp == kGroupWeight) {
       plan.m_blocks = (g.d_out + 255) / 256;
@@ -1164,11 +1172,12 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         const int cols0 = kOp == kGroupWeight ? columns(b) : round32(rows0);
         const bool two = L::kTileRows > L::kCols && kOp != kGroupWeight && rows1 > 0;
         const bool both = two || longer(b);
+        const int in_turn = longer(b) ? kLongBlocks - 1 : 0x3fffffff;  // K blocks of an accumulator, less 1: a power of two
         const uint32_t idesc = kIdesc | (static_cast<uint32_t>(cols0) >> 3 << 17);
         const uint32_t idesc1 = kIdesc | (static_cast<uint32_t>(round32(rows1)) >> 3 << 17);
         uint32_t d = 0;
         for (int kb = 0; kb < b.kb; ++kb) {
-          const bool first = longer(b) ? kb % kLongBlocks == 0 : kb % kChunk == 0;
+          const bool first = kLong ? (kb & in_turn) == 0 : kb % kChunk == 0;
           if (first) {
             const int buf = used & 1;
             if (!wait_pair<kAnywhere, R::kKeep>(&acc_empty[buf], ((used >> 1) & 1) ^ 1, abort_flag, g.status)) {
@@ -1205,7 +1214,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
               }
             }
           }
-          const bool last = kb + 1 == b.kb || (longer(b) ? (kb + 1) % kLongBlocks == 0 : (kb + 1) % kChunk == 0);
+          const bool last = kb + 1 == b.kb || (kLong ? ((kb + 1) & in_turn) == 0 : (kb + 1) % kChunk == 0);
           if (elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < kMmas; ++kk) {
@@ -1227,7 +1236,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
               }
             }
             if (last) pair_commit(&acc_full[used & 1]);
-            if (longer(b) && last) pair_commit(&acc_full[(used & 1) ^ 1]);
+            if (both && !two && last) pair_commit(&acc_full[(used & 1) ^ 1]);
             if (two) {  // the tile's other rows, against the same A
               const uint32_t lb1 = lb + cols0 / 2 * (128 / 16), d1 = tm + ((used & 1) ^ 1) * kAccCols;
 #pragma unroll
