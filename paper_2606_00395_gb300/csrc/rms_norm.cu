@@ -313,8 +313,9 @@ struct Ahead {
 };
 
 // A group of G threads walks rows.  The row stays packed as loaded between its sums and its gradient, so
-// that two blocks of 512 threads fit an SM; rows above 8192 are read twice, the second time from L2.  Each thread keeps the weight's gradient of its columns, which
-// the block's groups join at the end and weight_kernel over the blocks.
+// that two blocks of 512 threads fit an SM; rows above 8192 are read twice, the second time from L2.  Each
+// thread keeps the weight's gradient of its columns, which the block's groups join at the end and weight_kernel
+// over the blocks.
 //   ds = dsum + c1 (w dy) + c2 s,  c1 = rstd,  c2 = -rstd^3 (sum w dy s) / d,   dweight += (dy s) rstd
 template <int G>
 constexpr int kBackThreads = G < 512 ? 512 : G;
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(kBackThreads<G>, kBackThreads<G> == 512 ? 2 : 
   constexpr int kGroups = kThreads / G;
   constexpr int kWarps = G / 32;  // of a group
   constexpr bool kTwice = V > 1;
-  __shared__ float red[2][kThreads / 32][2];
+  __shared__ __align__(8) float red[2][kThreads / 32][2];  // a warp's sums, read as pairs
   __shared__ float join[kGroups > 1 ? kGroups : 1][kGroups > 1 ? G * 8 * V : 1];
   pdl_wait();
   pdl_trigger();
