@@ -78,7 +78,7 @@ constexpr int kMostMmas = 48, kExactMmas = 32, kKeepMmas = 16;
 // And that a result in 16 bits takes (16384 bf16 or 32768 e4m3 columns): 8e-5 of a sum of terms of one sign, 4 % of half
 // a step.  Longer sums (to one side 8e-4 at 131072 columns, 7e-3 at 2^20, where no value was rounded right) use one
 // accumulator and add it every so many MMAs to their sums in the other, whose epilogue then overlaps nothing (8192
-// rows, 8 matrices of 2048 x 32768: 666 us, as before; every 512 MMAs, 3e-5: 689).
+// rows, 8 matrices of 2048 x 32768: 681 us, without it 664; of 2048 x 16448 357, 343).
 constexpr int kLongMmas = 1024;
 
 // e4m3: K blocks (4096 columns) from which on up to 384 rows of an expert are one tile (see Plan)
@@ -311,33 +311,33 @@ __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uin
   }
 }
 
-// 16 columns of this lane into tensor memory, there for later loads of this warp after tmem_wait_st().
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// A warp's columns of an accumulator (16 of every 32, from c0 on) to, or onto, the sums.  Out of the way of the
-// epilogue's registers.
-static __device__ __noinline__ void add_chunk(uint32_t tacc, uint32_t tsum, int c0, int cols, bool add) {
+// A warp's columns of an accumulator (16 of every 32, from c0 on) to, or onto, the sums.  Four at a time: more take
+// registers that the rest of the epilogue needs (16: spills of 200 bytes, operands off 16 bytes 1 % slower).
+__device__ __forceinline__ void add_chunk(uint32_t tacc, uint32_t tsum, int c0, int cols, bool add) {
   for (; c0 < cols; c0 += 32) {
-    uint32_t v[16], sum[16];
-    tmem_ld16(tacc + c0, v);
-    if (add) tmem_ld16(tsum + c0, sum);
-    tmem_wait_ld(v);
-    if (add) {
-      reg_fence(sum);
+#pragma unroll 1
+    for (int c = c0; c < c0 + 16; c += 4) {
+      uint32_t v[4], w[4] = {0u, 0u, 0u, 0u};
+      auto load = [](uint32_t from, uint32_t (&r)[4]) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(from)
+                     : "memory");
+      };
+      load(tacc + c, v);
+      if (add) load(tsum + c, w);
+      asm volatile("tcgen05.wait::ld.sync.aligned;"
+                   : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3])
+                   :
+                   : "memory");
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(sum[j]));
+      for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+      asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tsum + c), "r"(v[0]), "r"(v[1]),
+                   "r"(v[2]), "r"(v[3])
+                   : "memory");
     }
-    tmem_st16(tsum + c0, v);
   }
-  tmem_wait_st();
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 // ---- jobs -------------------------------------------------------------------------------------
