@@ -10,8 +10,9 @@
 // A pair of CTAs computes 256 x 256 of D: each holds 128 rows of A and half of B in its shared memory
 // and 128 x 256 of D in its tensor memory, 32 KB of operands for 512 clk of MMA where one CTA alone
 // needs 48 KB (128 x 256) or has no room for a second accumulator (256 x 256).  The second accumulator
-// lets the epilogue of a tile overlap the MMAs of the next one.  Tiles of rows are N (a multiple of 32
-// up to 256), so an expert of few rows costs few MMAs and its matrix is read once per 256 rows.
+// lets the epilogue of a tile overlap the MMAs of the next one.  Tiles of rows are N, a multiple of 32, so an
+// expert of few rows costs few MMAs and its matrix is read once a tile: of up to 256 rows, or of up to 384 in
+// both accumulators without that overlap, where the expert has no more (see Plan).
 //
 // Warp roles: 0 TMA of A, 1 MMA (of the first CTA) and tensor memory, then (see Roles) TMA of B, epilogue, scheduler
 // and loaders, where there is something that TMA cannot bring: operands that do not start on 16 bytes (sixteen
@@ -19,9 +20,10 @@
 // the next expert's (four).  Every wait is bounded (pr2_device.cuh).
 //
 // The tensor core adds to its fp32 accumulator by cutting bits off, so the error of a long sum grows with
-// its length and to one side (8192 rows: 9e-6 of the norm, 512: 5e-7; fp32 FMAs in turn 3e-7).  Results in
-// fp32 therefore leave the accumulator every kMostMmas MMAs and are added up, rounded, where they are stored, by the
-// thread or the copies of the warp that stored them before; results in 16 bits every kLongMmas, in tensor memory.
+// its length and to one side (terms of any sign, 8192 rows: 9e-6 of the norm, 512: 5e-7, fp32 FMAs in turn 3e-7; terms
+// of one sign, 8192: 3.5e-5).  Results in fp32 therefore leave the accumulator every kMostMmas MMAs and are added up,
+// rounded, where they are stored, by the thread or the copies of the warp that stored them before; results in 16
+// bits every kLongMmas, in tensor memory.
 //
 // fp32 operands: each value is a sum of three bf16 values (24 bits), and eight of the nine products of their
 // planes, the first in an accumulator of its own, give the product to 2^-32 (see split3).
@@ -29,9 +31,9 @@
 // The launch has a pair for every job.  A pair that runs takes further jobs over from pairs that have not
 // started (cluster launch control), so that the pairs end at about the same time whatever the experts'
 // sizes, without a counter in memory.  The scheduler warps turn a pair's number into a job, once for all
-// roles.  Gradient of the matrices: the longest jobs first.  Forward and rows: experts in turn, because
-// jobs of one tile an expert wait for HBM and those of two for L2, and go better side by side (4096 tokens,
-// N = 128, k = 8: forward 226 us longest first, 214 in turn).
+// roles.  Gradient of the matrices: experts of most and of fewest rows in turn.  Forward and rows: as they are
+// numbered, because jobs of one tile an expert wait for HBM and those of two for L2, and go better side by side (4096
+// tokens, N = 128, k = 8: forward 226 us longest first, 214 as numbered).
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -705,7 +707,7 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
   pdl_wait();
   pdl_trigger();
 
-  // ---- the plan: experts' rows, in an order by the length of their jobs ----
+  // ---- the plan: weight: the experts' order by their rows; forward, rows: the jobs before each expert ----
   Plan<kOp, L> plan;
   {
     const int N = g.N, fours = (N + 3) & ~3, threads = static_cast<int>(blockDim.x);
