@@ -1174,7 +1174,8 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         const int cols0 = kOp == kGroupWeight ? columns(b) : round32(rows0);
         const bool two = L::kTileRows > L::kCols && kOp != kGroupWeight && rows1 > 0;
         const bool both = two || longer(b);
-        const int in_turn = longer(b) ? kLongBlocks - 1 : 0x3fffffff;  // K blocks of an accumulator, less 1: a power of two
+        // K blocks of an accumulator less one, as a mask
+        const int in_turn = longer(b) ? kLongBlocks - 1 : 0x3fffffff;
         const uint32_t idesc = kIdesc | (static_cast<uint32_t>(cols0) >> 3 << 17);
         const uint32_t idesc1 = kIdesc | (static_cast<uint32_t>(round32(rows1)) >> 3 << 17);
         uint32_t d = 0;
@@ -1287,7 +1288,8 @@ __global__ void __launch_bounds__(Roles<kOp, kType, kLoaders>::kThreads, 1)
         // The next job is taken when the loads of this one are nearly issued, not sooner: others may be free
         // before.  Behind a short one (an answer takes about 1.4 us) two are kept in hand.
         const int of = b.kb > kAskAhead ? n - 1 : n - 2;
-        if (rank == 0 && of >= 0) more = wait_pair<kHere, R::kKeep>(&want[of & 1], (of >> 1) & 1, abort_flag, g.status, limit);
+        if (rank == 0 && of >= 0)
+          more = wait_pair<kHere, R::kKeep>(&want[of & 1], (of >> 1) & 1, abort_flag, g.status, limit);
       }
       if (rank == 0) {
         if (asked > 0) more = wait_pair<kAnywhere, R::kKeep>(heard, (asked - 1) & 1, abort_flag, g.status) && more;
