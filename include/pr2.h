@@ -556,6 +556,8 @@ pr2_status pr2_grouped_gemm_weight_grad(const pr2_group_dims* dims, const void* 
  *  q [rows, d_in] (stride ld_in) and scale [rows] of pr2_rmsnorm or pr2_rows_to_8bit; Wq [N, d_out,
  *  d_in] e4m3 with a scale for each output channel, Wscale [N, d_out] fp32; y [rows, d_out] (stride
  *  ld_out) in dims->dtype.  Wq2, Wscale2 and y2 all or none.
+ *  Rows q of unsorted tokens go through pr2_token_sort as rows of d_in / 2 bf16 (or d_in / 4 fp32)
+ *  elements, their scales by its perm; widths that do not divide so are held in 8 bits after the sort.
  */
 pr2_status pr2_grouped_gemm_8bit(const pr2_group_dims* dims, const uint8_t* q, const float* scale,
                                  const uint8_t* Wq, const float* Wscale, const int32_t* offsets,
