@@ -76,7 +76,7 @@ constexpr int kMaxStages = 6;
 constexpr int kRawPitch = 144;                  // 128 bytes from anywhere in a 16-byte word: nine such words
 // MMAs in turn that a result in fp32 takes from one accumulator: of 16-bit operands 48 (relative error 7e-7; 32: 5e-7 and
 // an eighth more time for gradients of matrices of many rows); of fp32 ones, whose results should be as close as those
-// of fp32 FMAs, 16 (2.4e-7, FMAs 2.8e-7; 32: 4.8e-7 and 2 to 5 % less time); 16 where registers keep the sums.
+// of fp32 FMAs, 16 (2.4e-7, FMAs 2.8e-7; 32: 4.8e-7 and 2 to 11 % less time); 16 where registers keep the sums.
 constexpr int kMostMmas = 48, kExactMmas = 16, kKeepMmas = 16;
 // And that a result in 16 bits takes (16384 bf16 or 32768 e4m3 columns): 8e-5 of a sum of terms of one sign, 4 % of half
 // a step.  Longer sums (to one side 8e-4 at 131072 columns, 7e-3 at 2^20, where no value was rounded right) use one
